@@ -378,6 +378,100 @@ prc_status materialize_agent_kv(const lrsa_dims* dims, const uint16_t* K_base,
                                 uint16_t* K_full, uint16_t* V_full, void* stream);
 
 /*
+ * add_rms_norm -- the input of a layer's projections: the residual sum and its
+ * root-mean-square norm, row by row,
+ *     s = x[i] + residual[i],   residual_out[i] = s,
+ *     y[i] = s / sqrt(mean(s^2) + eps) * weight.
+ * Its y is the X of precompute_lr_cache, project_kv_and_lr_cache and
+ * adapted_projection.
+ *
+ *   x            [T, d] bf16, row stride ld_x (elements).
+ *   residual     [T, d] bf16, row stride ld_res, or NULL: s = x.
+ *   weight       [d] bf16.
+ *   residual_out [T, d] bf16, row stride ld_res_out: the residual of what
+ *                follows; NULL: not written.  It may be `residual` or `x`
+ *                itself (same pointer and row stride).
+ *   y            [T, d] bf16, row stride ld_y.  It may be `x` or `residual`
+ *                itself, unless residual_out is.
+ * Arithmetic: s, its mean of squares and the product in fp32; each output is
+ * rounded once (the norm is that of s, not of its rounding).  A row with a NaN
+ * or an infinity gives what these formulas give in fp32.
+ * Requires d % 8 == 0, 8 <= d <= 65536, row strides >= d and multiples of 8,
+ * eps >= 0 and finite, T < 2^31, and outputs that overlap no input and each
+ * other nowhere (but for the rows in place above).  T == 0 is a no-op.
+ */
+prc_status add_rms_norm(const uint16_t* x, int64_t T, int64_t d, int64_t ld_x, const uint16_t* residual,
+                        int64_t ld_res, const uint16_t* weight, float eps, uint16_t* residual_out,
+                        int64_t ld_res_out, uint16_t* y, int64_t ld_y, void* stream);
+
+/*
+ * add_rms_norm_fp8 -- add_rms_norm with y in 8 bits, as
+ * adapted_projection_fp8 reads it: row i holds
+ *     y_scale[i] = max(max_j |y[i][j]|, 2^-100) / 448,
+ *     y8[i][j]   = e4m3(y[i][j] / y_scale[i])   (round to nearest even).
+ * A row with a NaN gets a NaN scale.
+ *   y        [T, d] e4m3 (OCP, finite and NaN), row stride ld_y, must overlap
+ *            no input.
+ *   y_scale  [T] fp32.
+ * Requires d % 16 == 0 and ld_y % 16 == 0 besides.
+ */
+prc_status add_rms_norm_fp8(const uint16_t* x, int64_t T, int64_t d, int64_t ld_x, const uint16_t* residual,
+                            int64_t ld_res, const uint16_t* weight, float eps, uint16_t* residual_out,
+                            int64_t ld_res_out, uint8_t* y, int64_t ld_y, float* y_scale, void* stream);
+
+/*
+ * adapted_projection -- a projection that is not cached (q_proj in the paper's
+ * default QV wiring, q_proj and o_proj in QKVO; Sec. 4.1, App. D.2) of rows
+ * that belong to many agents, each with its own adapter (Eq. 1):
+ *     Y[i] = X[i] W + (X[i] A_a) B_a,   a = agent[i].
+ *
+ *   X        [T, d_in] bf16, row stride ld_x (elements).
+ *   W        [d_in, d_out] bf16, contiguous.
+ *   A_stack  [d_in, N*r] bf16, contiguous: columns [a*r, (a+1)*r) hold agent
+ *            a's A (as for precompute_lr_cache with one projection).
+ *   B        [N, r, d_out] bf16, contiguous: each agent's up-projection.
+ *   agent    [T] int32, DEVICE memory, in any order.  A row whose entry is
+ *            negative takes the base projection alone; so does one at or past
+ *            N, which the checked build reports (PRC_EDEVDATA).
+ *   Y        [T, d_out] bf16, row stride ld_y; must overlap no input.
+ *   n_agents == 0: X W for every row; A_stack, B and agent may be NULL and
+ *            rank is ignored.
+ *   workspace  device scratch of at least adapted_projection_workspace_size
+ *            bytes (NULL allowed when the size is 0), 16-byte aligned.
+ *            Contents need no initialisation; calls that share a workspace
+ *            must be ordered on one stream.
+ * Arithmetic: bf16 inputs, fp32 sums; X A_a is rounded to bf16 (as the LR
+ * caches hold it) before its product with B_a; Y is rounded once.  What is
+ * infinite or NaN in one agent's A or B, or in one row of X, stays in the rows
+ * that use it.  The same call gives the same bits.
+ * Requires d_in, d_out, ld_x, ld_y multiples of 8, r in {8, 16, 32, 64},
+ * ld_x and ld_y at least d_in and d_out and below 2^22, T < 2^31 and d_in * d_out, d_in * N * r
+ * below 2^30 - 2^20 (PRC_EUNSUPPORTED otherwise).  T == 0 is a no-op.
+ */
+prc_status adapted_projection(const uint16_t* X, int64_t T, int64_t d_in, int64_t ld_x, const uint16_t* W,
+                              int64_t d_out, const uint16_t* A_stack, const uint16_t* B, int32_t n_agents,
+                              int32_t rank, const int32_t* agent, uint16_t* Y, int64_t ld_y, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/*
+ * adapted_projection_fp8 -- adapted_projection with X and W in 8 bits (e4m3,
+ * OCP): X[i][k] stands for x_scale[i] * X8[i][k] (as add_rms_norm_fp8 writes
+ * it) and W[k][j] for w_scale[j] * W8[k][j].  A_stack, B and Y stay bf16.
+ *   X  [T, d_in] e4m3, W [d_in, d_out] e4m3, x_scale [T] and w_scale [d_out]
+ *   fp32.
+ * Requires d_in, d_out and ld_x multiples of 16 besides.
+ */
+prc_status adapted_projection_fp8(const uint8_t* X, const float* x_scale, int64_t T, int64_t d_in, int64_t ld_x,
+                                  const uint8_t* W, const float* w_scale, int64_t d_out, const uint16_t* A_stack,
+                                  const uint16_t* B, int32_t n_agents, int32_t rank, const int32_t* agent,
+                                  uint16_t* Y, int64_t ld_y, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+
+/* Workspace bytes that adapted_projection and adapted_projection_fp8 need (0
+ * when none, or when the sizes are invalid; the calls report those). */
+size_t adapted_projection_workspace_size(int64_t T, int64_t d_in, int64_t d_out, int32_t n_agents, int32_t rank);
+
+/*
  * prc_stream_read -- measurement helper, not part of the hot path: reads
  * `bytes` bytes of device memory at `src` with 16-byte loads from `grid`
  * workgroups of 256 threads (grid-stride) and writes one XOR word per

@@ -9,6 +9,11 @@ from .binding import (  # noqa: F401
     LrsaDims,
     LrsaPaging,
     PrecacheError,
+    adapted_projection,
+    adapted_projection_fp8,
+    adapted_projection_workspace_size,
+    add_rms_norm,
+    add_rms_norm_fp8,
     lib,
     lr_shared_attention,
     lr_shared_attention_noalloc,

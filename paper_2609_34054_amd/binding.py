@@ -30,7 +30,8 @@ STATUS_NAMES = {0: "PRC_OK", 1: "PRC_EINVAL", 2: "PRC_ESHAPE", 3: "PRC_EALIGN",
 EXPORTS = ("precompute_lr_cache", "project_kv_and_lr_cache", "project_kv_and_lr_cache_paged",
            "lr_shared_attention", "lr_shared_attention_workspace_size", "lr_shared_attention_paged",
            "lr_shared_attention_paged_workspace_size", "lr_shared_attention_noalloc", "materialize_agent_kv",
-           "prc_stream_read", "prc_last_error",
+           "add_rms_norm", "add_rms_norm_fp8", "adapted_projection", "adapted_projection_fp8",
+           "adapted_projection_workspace_size", "prc_stream_read", "prc_last_error",
            "prc_status_string", "prc_version", "prc_device_checks")
 
 
@@ -109,6 +110,18 @@ def lib() -> ctypes.CDLL:
         L.lr_shared_attention_paged_workspace_size.restype = ctypes.c_size_t
         L.materialize_agent_kv.argtypes = [ctypes.POINTER(LrsaDims), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.materialize_agent_kv.restype = ctypes.c_int
+        norm = [vp, i64, i64, i64, vp, i64, vp, ctypes.c_float, vp, i64, vp, i64]
+        L.add_rms_norm.argtypes = norm + [vp]
+        L.add_rms_norm.restype = ctypes.c_int
+        L.add_rms_norm_fp8.argtypes = norm + [vp, vp]
+        L.add_rms_norm_fp8.restype = ctypes.c_int
+        adapters = [vp, vp, i32, i32, vp, vp, i64, vp, ctypes.c_size_t, vp]
+        L.adapted_projection.argtypes = [vp, i64, i64, i64, vp, i64] + adapters
+        L.adapted_projection.restype = ctypes.c_int
+        L.adapted_projection_fp8.argtypes = [vp, vp, i64, i64, i64, vp, vp, i64] + adapters
+        L.adapted_projection_fp8.restype = ctypes.c_int
+        L.adapted_projection_workspace_size.argtypes = [i64, i64, i64, i32, i32]
+        L.adapted_projection_workspace_size.restype = ctypes.c_size_t
         L.prc_stream_read.argtypes = [vp, ctypes.c_size_t, vp, i32, vp]
         L.prc_stream_read.restype = ctypes.c_int
         L.prc_last_error.restype = ctypes.c_char_p
@@ -565,6 +578,179 @@ def lr_shared_attention_paged(Q, K_pool, V_pool, L_k, L_v, B_k, B_v, positions, 
                                          ws_bytes, _stream(stream))
     _check("lr_shared_attention_paged", st)
     return O, lse
+
+
+def _one_device(func: str, tensors) -> torch.device:
+    """The GPU that holds every tensor of a call."""
+    dev = None
+    for name, t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{func}: {name} is on {t.device}, not on a GPU")
+        if dev is not None and t.device != dev:
+            raise ValueError(f"{func}: {name} is on {t.device}, other tensors on {dev}")
+        dev = t.device
+    return dev
+
+
+def _rows(name, t, dtype, shape, contiguous=False):
+    """A 2-D tensor of rows: dtype, shape, and elements of a row side by side."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {str(dtype)[6:]}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} shape {tuple(t.shape)} is not {tuple(shape)}")
+    if (t.numel() and t.stride(-1) != 1) or (contiguous and not t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous" + ("" if contiguous else " in its last dimension"))
+
+
+def _ld(t):
+    """Row stride; a single row's is its width (whatever the tensor says)."""
+    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 15) // 16 * 16
+
+
+def _norm(func, x, weight, residual, eps, y, y_scale, residual_out, fp8, stream):
+    kind = torch.float8_e4m3fn if fp8 else torch.bfloat16
+    if _on_gpu(x) and x.dim() == 2:
+        nat = _native()
+        if y is None:
+            y = torch.empty(x.shape, dtype=kind, device=x.device)
+        if fp8 and y_scale is None:
+            y_scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+        if residual is not None and residual_out is None:
+            residual_out = torch.empty_like(residual, memory_format=torch.contiguous_format)
+        st = nat.m.norm(getattr(nat, func), fp8, x, weight, residual, eps, residual_out, y, y_scale,
+                        torch._C._cuda_getDevice(), _raw_stream(stream))
+        if st is not None:
+            if st:
+                _check(func, st)
+            return y, y_scale, residual_out
+    _bf16("x", x, 2)
+    T, d = x.shape
+    _rows("weight", weight, torch.bfloat16, (d,))
+    if residual is not None:
+        _rows("residual", residual, torch.bfloat16, (T, d))
+    if y is None:
+        y = torch.empty((T, d), dtype=kind, device=x.device)
+    if fp8 and y_scale is None:
+        y_scale = torch.empty(T, dtype=torch.float32, device=x.device)
+    if residual is not None and residual_out is None:
+        residual_out = torch.empty((T, d), dtype=torch.bfloat16, device=x.device)
+    _rows("y", y, kind, (T, d))
+    if fp8:
+        _rows("y_scale", y_scale, torch.float32, (T,))
+    if residual_out is not None:
+        _rows("residual_out", residual_out, torch.bfloat16, (T, d))
+    dev = _one_device(func, (("x", x), ("weight", weight), ("residual", residual), ("residual_out", residual_out),
+                             ("y", y), ("y_scale", y_scale)))
+    args = [_ptr(x), T, d, _ld(x), _ptr(residual), 0 if residual is None else _ld(residual), _ptr(weight), float(eps),
+            _ptr(residual_out), 0 if residual_out is None else _ld(residual_out), _ptr(y), _ld(y)]
+    with torch.cuda.device(dev):
+        _check(func, getattr(lib(), func)(*args, *((_ptr(y_scale),) if fp8 else ()), _stream(stream)))
+    return y, y_scale, residual_out
+
+
+def add_rms_norm(x, weight, residual=None, *, eps: float = 1e-5, y=None, residual_out=None, stream=None):
+    """Residual sum and RMS norm of a layer input: ``s = x + residual``,
+    ``y = s / sqrt(mean(s**2) + eps) * weight`` per row.
+
+    ``x, residual [T, d]`` (row strides may exceed d) and ``weight [d]`` bf16.
+    Returns ``(y, residual_out)``, ``residual_out`` holding s (None without a
+    residual, unless one is given to write to; it may be ``residual`` itself).
+    """
+    y, _, out = _norm("add_rms_norm", x, weight, residual, eps, y, None, residual_out, False, stream)
+    return y, out
+
+
+def add_rms_norm_fp8(x, weight, residual=None, *, eps: float = 1e-5, y=None, y_scale=None, residual_out=None,
+                     stream=None):
+    """:func:`add_rms_norm` with y in 8 bits: ``y [T, d]`` float8_e4m3fn and
+    ``y_scale [T]`` fp32, row i standing for ``y[i] * y_scale[i]`` (the largest
+    value of a row is 448 before its scale).  Returns ``(y, y_scale, residual_out)``."""
+    return _norm("add_rms_norm_fp8", x, weight, residual, eps, y, y_scale, residual_out, True, stream)
+
+
+def adapted_projection_workspace_size(T: int, d_in: int, d_out: int, n_agents: int, rank: int) -> int:
+    return int(lib().adapted_projection_workspace_size(T, d_in, d_out, n_agents, rank))
+
+
+def _adapted(func, X, x_scale, W, w_scale, A_stack, B, agent, Y, workspace, stream):
+    fp8 = func == "adapted_projection_fp8"
+    if _on_gpu(X) and W.dim() == 2 and X.dim() == 2:
+        nat = _native()
+        out, ws, raw = Y, workspace, _raw_stream(stream)
+        if out is None:
+            out = torch.empty((X.shape[0], W.shape[1]), dtype=torch.bfloat16, device=X.device)
+        while True:
+            st = nat.m.adapted(getattr(nat, func), nat.adapted_projection_workspace_size, fp8, X, x_scale, W, w_scale,
+                               A_stack, B, agent, out, ws, torch._C._cuda_getDevice(), raw)
+            if type(st) is not tuple:
+                break
+            ws = torch.empty(st[0], dtype=torch.uint8, device=X.device)
+        if st is not None:
+            if st:
+                _check(func, st)
+            return out
+    kind = torch.float8_e4m3fn if fp8 else torch.bfloat16
+    if X.dim() != 2 or W.dim() != 2:
+        raise ValueError(f"X and W must have 2 dims, got shapes {tuple(X.shape)}, {tuple(W.shape)}")
+    (T, d_in), d_out = X.shape, W.shape[1]
+    _rows("X", X, kind, (T, d_in))
+    _rows("W", W, kind, (d_in, d_out), contiguous=True)
+    if fp8:
+        _rows("x_scale", x_scale, torch.float32, (T,))
+        _rows("w_scale", w_scale, torch.float32, (d_out,))
+    given = [t is not None for t in (A_stack, B, agent)]
+    if any(given) != all(given):
+        raise ValueError("A_stack, B and agent must be given together")
+    n_agents = rank = 0
+    if B is not None:
+        if B.dim() != 3:
+            raise ValueError(f"B must have 3 dims, got shape {tuple(B.shape)}")
+        n_agents, rank = B.shape[:2]
+        _rows("B", B, torch.bfloat16, (n_agents, rank, d_out), contiguous=True)
+        _rows("A_stack", A_stack, torch.bfloat16, (d_in, n_agents * rank), contiguous=True)
+        _rows("agent", agent, torch.int32, (T,))
+    if Y is None:
+        Y = torch.empty((T, d_out), dtype=torch.bfloat16, device=X.device)
+    _rows("Y", Y, torch.bfloat16, (T, d_out))
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    dev = _one_device(func, (("X", X), ("x_scale", x_scale), ("W", W), ("w_scale", w_scale), ("A_stack", A_stack),
+                             ("B", B), ("agent", agent), ("Y", Y), ("workspace", workspace)))
+    with torch.cuda.device(dev):
+        need = adapted_projection_workspace_size(T, d_in, d_out, n_agents, rank)
+        if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        tail = [_ptr(A_stack), _ptr(B), n_agents, rank, _ptr(agent), _ptr(Y), _ld(Y), _ptr(workspace), ws_bytes,
+                _stream(stream)]
+        if fp8:
+            st = lib().adapted_projection_fp8(_ptr(X), _ptr(x_scale), T, d_in, _ld(X), _ptr(W), _ptr(w_scale), d_out, *tail)
+        else:
+            st = lib().adapted_projection(_ptr(X), T, d_in, _ld(X), _ptr(W), d_out, *tail)
+    _check(func, st)
+    return Y
+
+
+def adapted_projection(X, W, A_stack, B, agent, *, Y=None, workspace=None, stream=None):
+    """``Y[i] = X[i] @ W + (X[i] @ A_a) @ B_a`` with ``a = agent[i]``: a projection
+    whose rows belong to many agents, each with its own adapter (Eq. 1).
+
+    ``X [T, d_in]`` bf16 (row stride may exceed d_in), ``W [d_in, d_out]``,
+    ``A_stack [d_in, N*r]``, ``B [N, r, d_out]`` bf16 contiguous; ``agent [T]``
+    int32, entries outside [0, N) (use -1) taking the base projection alone.
+    ``A_stack``, ``B`` and ``agent`` None: ``X @ W``.  A workspace is allocated
+    when none (or too small a one) is given.
+    """
+    return _adapted("adapted_projection", X, None, W, None, A_stack, B, agent, Y, workspace, stream)
+
+
+def adapted_projection_fp8(X, x_scale, W, w_scale, A_stack, B, agent, *, Y=None, workspace=None, stream=None):
+    """:func:`adapted_projection` with X and W in 8 bits: ``X [T, d_in]`` and
+    ``W [d_in, d_out]`` float8_e4m3fn, ``x_scale [T]`` (as
+    :func:`add_rms_norm_fp8` writes them) and ``w_scale [d_out]`` fp32."""
+    return _adapted("adapted_projection_fp8", X, x_scale, W, w_scale, A_stack, B, agent, Y, workspace, stream)
 
 
 def stream_read(src, sink, grid: int, stream=None):

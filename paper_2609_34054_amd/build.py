@@ -27,6 +27,8 @@ MARSHAL_PATH = os.path.join(PKG, "_marshal.so")
 SOURCES = [
     "abi.cpp",
     "precompute_gemm.hip",
+    "adapted_projection.hip",
+    "rms_norm.hip",
     "lrsa_decode.hip",
     "lrsa_prefill.hip",
     "materialize.hip",

@@ -741,6 +741,204 @@ PRC_API prc_status materialize_agent_kv(const lrsa_dims* dims, const uint16_t* K
   return launch_status(prc::launch_materialize(c.a, static_cast<hipStream_t>(stream)), "materialize_agent_kv");
 }
 
+namespace {
+
+// Extent of a [rows, cols] array with row stride ld, in bytes.
+struct Span {
+  const char* name;
+  const void* p;
+  uintptr_t bytes;
+};
+Span span(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t elem) {
+  return {name, p, p == nullptr ? 0 : (uintptr_t)(((rows - 1) * ld + cols) * elem)};
+}
+bool overlap(const Span& a, const Span& b) {
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+  return a.bytes > 0 && b.bytes > 0 && a0 < b0 + b.bytes && b0 < a0 + a.bytes;
+}
+
+// Shared body of the two forms of add_rms_norm; elem: bytes of an element of y.
+prc_status norm_impl(const char* who, const uint16_t* x, int64_t T, int64_t d, int64_t ld_x, const uint16_t* residual,
+                     int64_t ld_res, const uint16_t* weight, float eps, uint16_t* residual_out, int64_t ld_ro, void* y,
+                     int64_t ld_y, float* y_scale, int elem, hipStream_t stream) {
+  if (T < 0 || T > INT32_MAX) return fail(PRC_EINVAL, "T=%lld outside [0, 2^31)", (long long)T);
+  const int step = elem == 1 ? 16 : 8;
+  if (d < 8 || d > 65536 || d % step)
+    return fail(PRC_EUNSUPPORTED, "d=%lld must be a multiple of %d in [8, 65536]", (long long)d, step);
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(PRC_EINVAL, "eps=%g must be finite and not negative", (double)eps);
+  struct {
+    const char* name;
+    int64_t ld;
+    bool used;
+    int step;
+  } lds[] = {{"ld_x", ld_x, true, 8},
+             {"ld_res", ld_res, residual != nullptr, 8},
+             {"ld_res_out", ld_ro, residual_out != nullptr, 8},
+             {"ld_y", ld_y, true, step}};
+  for (const auto& l : lds) {
+    if (!l.used) continue;
+    if (l.ld < d || l.ld >= (1LL << 40)) return fail(PRC_ESHAPE, "%s=%lld outside [d=%lld, 2^40)", l.name, (long long)l.ld, (long long)d);
+    if (l.ld % l.step) return fail(PRC_EALIGN, "%s=%lld is not a multiple of %d elements", l.name, (long long)l.ld, l.step);
+  }
+  if (T == 0) return ok();
+  if (x == nullptr || weight == nullptr || y == nullptr || (elem == 1 && y_scale == nullptr))
+    return fail(PRC_EINVAL, elem == 1 ? "x/weight/y/y_scale is NULL" : "x/weight/y is NULL");
+  if (!aligned(x, 16) || !aligned(weight, 16) || !aligned(y, 16) || !aligned(residual, 16) || !aligned(residual_out, 16))
+    return fail(PRC_EALIGN, "x/residual/weight/residual_out/y must be 16-byte aligned");
+  if (!aligned(y_scale, 4)) return fail(PRC_EALIGN, "y_scale is not 4-byte aligned");
+  // Outputs overlap nothing, but a row may be written where the same row was
+  // read (its threads have all read it before any of them writes).
+  const Span in[] = {span("x", x, T, d, ld_x, 2), span("residual", residual, T, d, ld_res, 2), span("weight", weight, 1, d, d, 2)};
+  const int64_t in_ld[] = {ld_x, ld_res, 0};
+  const Span out[] = {span("residual_out", residual_out, T, d, ld_ro, 2), span("y", y, T, d, ld_y, elem),
+                      span("y_scale", y_scale, 1, T, T, 4)};
+  const int64_t out_ld[] = {ld_ro, elem == 2 ? ld_y : -1, -1};
+  for (int o = 0; o < 3; ++o) {
+    for (int i = 0; i < 3; ++i) {
+      const bool in_place = out[o].p == in[i].p && out_ld[o] == in_ld[i];
+      if (overlap(out[o], in[i]) && !in_place) return fail(PRC_EINVAL, "%s overlaps %s", out[o].name, in[i].name);
+    }
+    for (int p = 0; p < o; ++p)
+      if (overlap(out[o], out[p])) return fail(PRC_EINVAL, "%s overlaps %s", out[o].name, out[p].name);
+  }
+  prc::NormArgs a{};
+  a.x = x;
+  a.residual = residual;
+  a.weight = weight;
+  a.residual_out = residual_out;
+  a.y = y;
+  a.y_scale = y_scale;
+  a.T = T;
+  a.ld_x = ld_x;
+  a.ld_res = ld_res;
+  a.ld_ro = ld_ro;
+  a.ld_y = ld_y;
+  a.d = (int32_t)d;
+  a.eps = eps;
+  int cus = 0;
+  if (prc_status ds = device_ready(&cus)) return ds;
+  return launch_status(prc::launch_rms_norm(a, stream), who);
+}
+
+// Limits that the workspace query and the call share.
+prc_status check_projection(int64_t T, int64_t d_in, int64_t d_out, int32_t n_agents, int32_t rank, int step) {
+  if (T < 0 || T > INT32_MAX) return fail(PRC_EINVAL, "T=%lld outside [0, 2^31)", (long long)T);
+  if (d_in < 1 || d_in % step || d_out < 1 || d_out % step)
+    return fail(PRC_EUNSUPPORTED, "d_in=%lld, d_out=%lld must be positive multiples of %d", (long long)d_in, (long long)d_out, step);
+  if (n_agents < 0) return fail(PRC_EINVAL, "n_agents=%d is negative", n_agents);
+  if (n_agents > 0 && !rank_ok(rank)) return fail(PRC_EUNSUPPORTED, "rank=%d (built: 8, 16, 32, 64)", rank);
+  // Weights are addressed with 32-bit byte offsets.
+  const int64_t most = (1LL << 30) - (1LL << 20);
+  if (d_in >= (1LL << 22) || d_out >= (1LL << 22) || d_in * d_out > most)
+    return fail(PRC_EUNSUPPORTED, "d_in=%lld times d_out=%lld weights are too many", (long long)d_in, (long long)d_out);
+  if (n_agents > 0 && d_in * n_agents > most / rank)
+    return fail(PRC_EUNSUPPORTED, "d_in=%lld times %d adapters of rank %d are too many", (long long)d_in, n_agents, rank);
+  return PRC_OK;
+}
+
+// Shared body of the two forms of adapted_projection; elem: bytes of an
+// element of X and W.
+prc_status adapted_impl(const char* who, const void* X, const float* x_scale, int64_t T, int64_t d_in, int64_t ld_x,
+                        const void* W, const float* w_scale, int64_t d_out, const uint16_t* A_stack, const uint16_t* B,
+                        int32_t n_agents, int32_t rank, const int32_t* agent, uint16_t* Y, int64_t ld_y, int elem,
+                        void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const int step = elem == 1 ? 16 : 8;
+  if (prc_status s = check_projection(T, d_in, d_out, n_agents, rank, step)) return s;
+  if (ld_x < d_in || ld_y < d_out)
+    return fail(PRC_ESHAPE, "ld_x=%lld, ld_y=%lld are below d_in=%lld, d_out=%lld", (long long)ld_x, (long long)ld_y,
+                (long long)d_in, (long long)d_out);
+  if (ld_x >= (1LL << 22) || ld_y >= (1LL << 22))
+    return fail(PRC_EUNSUPPORTED, "ld_x=%lld, ld_y=%lld must be below 2^22", (long long)ld_x, (long long)ld_y);
+  if (ld_x % step || ld_y % 8)
+    return fail(PRC_EALIGN, "ld_x=%lld, ld_y=%lld are not multiples of %d, 8 elements", (long long)ld_x, (long long)ld_y, step);
+  if (T == 0) return ok();
+  const bool lr = n_agents > 0;
+  if (X == nullptr || W == nullptr || Y == nullptr || (lr && (A_stack == nullptr || B == nullptr || agent == nullptr)))
+    return fail(PRC_EINVAL, "X/W/A_stack/B/agent/Y is NULL");
+  if (elem == 1 && (x_scale == nullptr || w_scale == nullptr)) return fail(PRC_EINVAL, "x_scale/w_scale is NULL");
+  if (!aligned(X, 16) || !aligned(W, 16) || !aligned(Y, 16) || (lr && (!aligned(A_stack, 16) || !aligned(B, 16))))
+    return fail(PRC_EALIGN, "X/W/A_stack/B/Y must be 16-byte aligned");
+  if (!aligned(x_scale, 4) || !aligned(w_scale, 4) || (lr && !aligned(agent, 4)))
+    return fail(PRC_EALIGN, "x_scale/w_scale/agent are not 4-byte aligned");
+  const int64_t cols = lr ? (int64_t)n_agents * rank : 0;
+  const size_t need = adapted_projection_workspace_size(T, d_in, d_out, n_agents, rank);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need))
+    return fail(PRC_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace == nullptr ? 0 : workspace_bytes, need);
+  if (need > 0 && !aligned(workspace, 16)) return fail(PRC_EALIGN, "workspace is not 16-byte aligned");
+  const Span in[] = {span("X", X, T, d_in, ld_x, elem),
+                     span("W", W, d_in, d_out, d_out, elem),
+                     span("x_scale", x_scale, 1, T, T, 4),
+                     span("w_scale", w_scale, 1, d_out, d_out, 4),
+                     span("A_stack", lr ? A_stack : nullptr, d_in, cols, cols, 2),
+                     span("B", lr ? B : nullptr, cols, d_out, d_out, 2),
+                     span("agent", lr ? agent : nullptr, 1, T, T, 4)};
+  const Span out[] = {span("Y", Y, T, d_out, ld_y, 2), {"workspace", need > 0 ? workspace : nullptr, need}};
+  for (const Span& o : out)
+    for (const Span& i : in)
+      if (overlap(o, i)) return fail(PRC_EINVAL, "%s overlaps %s", o.name, i.name);
+  if (overlap(out[0], out[1])) return fail(PRC_EINVAL, "Y overlaps workspace");
+  prc::ProjectArgs a{};
+  a.X = X;
+  a.W = W;
+  a.x_scale = elem == 1 ? x_scale : nullptr;
+  a.w_scale = elem == 1 ? w_scale : nullptr;
+  a.A = A_stack;
+  a.B = B;
+  a.agent = agent;
+  a.Y = Y;
+  a.ws = workspace;
+  a.T = T;
+  a.d_in = d_in;
+  a.d_out = d_out;
+  a.ld_x = ld_x;
+  a.ld_y = ld_y;
+  a.n_agents = n_agents;
+  a.rank = lr ? rank : 8;
+  int cus = 0;
+  if (prc_status ds = device_ready(&cus)) return ds;
+  a.cus = cus;
+  return launch_status(prc::launch_adapted_projection(a, stream), who);
+}
+
+}  // namespace
+
+PRC_API prc_status add_rms_norm(const uint16_t* x, int64_t T, int64_t d, int64_t ld_x, const uint16_t* residual,
+                                int64_t ld_res, const uint16_t* weight, float eps, uint16_t* residual_out,
+                                int64_t ld_res_out, uint16_t* y, int64_t ld_y, void* stream) {
+  return norm_impl("add_rms_norm", x, T, d, ld_x, residual, ld_res, weight, eps, residual_out, ld_res_out, y, ld_y, nullptr,
+                   2, static_cast<hipStream_t>(stream));
+}
+
+PRC_API prc_status add_rms_norm_fp8(const uint16_t* x, int64_t T, int64_t d, int64_t ld_x, const uint16_t* residual,
+                                    int64_t ld_res, const uint16_t* weight, float eps, uint16_t* residual_out,
+                                    int64_t ld_res_out, uint8_t* y, int64_t ld_y, float* y_scale, void* stream) {
+  return norm_impl("add_rms_norm_fp8", x, T, d, ld_x, residual, ld_res, weight, eps, residual_out, ld_res_out, y, ld_y,
+                   y_scale, 1, static_cast<hipStream_t>(stream));
+}
+
+PRC_API prc_status adapted_projection(const uint16_t* X, int64_t T, int64_t d_in, int64_t ld_x, const uint16_t* W,
+                                      int64_t d_out, const uint16_t* A_stack, const uint16_t* B, int32_t n_agents,
+                                      int32_t rank, const int32_t* agent, uint16_t* Y, int64_t ld_y, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
+  return adapted_impl("adapted_projection", X, nullptr, T, d_in, ld_x, W, nullptr, d_out, A_stack, B, n_agents, rank, agent,
+                      Y, ld_y, 2, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+PRC_API prc_status adapted_projection_fp8(const uint8_t* X, const float* x_scale, int64_t T, int64_t d_in, int64_t ld_x,
+                                          const uint8_t* W, const float* w_scale, int64_t d_out, const uint16_t* A_stack,
+                                          const uint16_t* B, int32_t n_agents, int32_t rank, const int32_t* agent,
+                                          uint16_t* Y, int64_t ld_y, void* workspace, size_t workspace_bytes, void* stream) {
+  return adapted_impl("adapted_projection_fp8", X, x_scale, T, d_in, ld_x, W, w_scale, d_out, A_stack, B, n_agents, rank,
+                      agent, Y, ld_y, 1, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+PRC_API size_t adapted_projection_workspace_size(int64_t T, int64_t d_in, int64_t d_out, int32_t n_agents, int32_t rank) {
+  if (T < 1 || T > INT32_MAX || d_in < 1 || d_out < 1 || d_in >= (1LL << 22) || d_out >= (1LL << 22) || n_agents < 0 ||
+      (n_agents > 0 && !rank_ok(rank)))
+    return 0;
+  return prc::adapted_projection_bytes(T, d_in, d_out, n_agents, rank, plan_cus());
+}
+
 PRC_API prc_status prc_stream_read(const void* src, size_t bytes, uint32_t* sink, int32_t grid, void* stream) {
   if (src == nullptr || sink == nullptr) return fail(PRC_EINVAL, "src/sink is NULL");
   if (bytes == 0 || bytes % 16 || bytes > ((size_t)1 << 40)) return fail(PRC_EINVAL, "bytes=%zu must be a positive multiple of 16", bytes);

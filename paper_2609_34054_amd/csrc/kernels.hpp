@@ -158,6 +158,41 @@ struct PrecomputeArgs {
 };
 hipError_t launch_precompute(const PrecomputeArgs& a, hipStream_t stream);
 
+// Residual sum and RMS norm of a layer input (strides in elements).
+struct NormArgs {
+  const uint16_t* x;         // [T, d]
+  const uint16_t* residual;  // [T, d], or nullptr
+  const uint16_t* weight;    // [d]
+  uint16_t* residual_out;    // [T, d], or nullptr
+  void* y;                   // [T, d] bf16, or e4m3 with y_scale
+  float* y_scale;            // [T], or nullptr: bf16
+  int64_t T;
+  int64_t ld_x, ld_res, ld_ro, ld_y;
+  int32_t d;
+  float eps;
+};
+hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream);
+
+// Projection with each row's adapter.
+struct ProjectArgs {
+  const void* X;            // [T, d_in] bf16, or e4m3 with x_scale
+  const void* W;            // [d_in, d_out] bf16, or e4m3 with w_scale
+  const float* x_scale;     // [T], or nullptr: bf16
+  const float* w_scale;     // [d_out]
+  const uint16_t* A;        // [d_in, n_agents * rank]
+  const uint16_t* B;        // [n_agents, rank, d_out]
+  const int32_t* agent;     // [T]
+  uint16_t* Y;              // [T, d_out]
+  void* ws;
+  int64_t T, d_in, d_out;
+  int64_t ld_x, ld_y;       // elements
+  int32_t n_agents;         // 0: X W alone
+  int32_t rank;
+  int32_t cus;
+};
+size_t adapted_projection_bytes(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, int cus);
+hipError_t launch_adapted_projection(const ProjectArgs& a, hipStream_t stream);
+
 // Measurement helper: stream `bytes` (a multiple of 16) from src with `grid`
 // workgroups, one XOR word per workgroup to sink.
 hipError_t launch_stream_read(const void* src, int64_t bytes, uint32_t* sink, int grid, hipStream_t stream);

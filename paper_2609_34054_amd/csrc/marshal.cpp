@@ -337,6 +337,100 @@ PyObject* project_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong((long)st);
 }
 
+// Whether `t` holds rows of `cols` elements of `type`, on device `dev`.
+bool rows_of(const Tensor* t, at::ScalarType type, int64_t rows, int64_t cols, int64_t dev) {
+  return t->scalar_type() == type && t->dim() == 2 && t->size(0) == rows && t->size(1) == cols && t->stride(1) == 1 &&
+         t->get_device() == dev;
+}
+bool vector_of(const Tensor* t, at::ScalarType type, int64_t n, int64_t dev) {
+  return t->scalar_type() == type && t->dim() == 1 && t->size(0) == n && t->is_contiguous() && t->get_device() == dev;
+}
+// Row stride in elements; of a single row, its width rounded to 16 elements.
+int64_t row_stride(const Tensor* t) { return t == nullptr ? 0 : t->size(0) > 1 ? t->stride(0) : (t->size(1) + 15) / 16 * 16; }
+
+// norm(fn, fp8, x, weight, residual, eps, residual_out, y, y_scale, device, stream)
+PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 11) return none();
+  void *fn, *stream;
+  const bool fp8 = a[1] == Py_True;
+  const Tensor *x = tensor(a[2]), *w = tensor(a[3]), *y = tensor(a[7]), *res, *ro, *ys;
+  double eps;
+  int64_t dev;
+  if (!as_ptr(a[0], &fn) || !as_ptr(a[10], &stream) || !x || !w || !y || !opt(a[4], &res) || !opt(a[6], &ro) ||
+      !opt(a[8], &ys) || !as_double(a[5], &eps) || !as_int(a[9], &dev))
+    return none();
+  if (!bf16(x, 2) || x->get_device() != dev) return none();
+  const int64_t T = x->size(0), d = x->size(1);
+  if (!vector_of(w, at::kBFloat16, d, dev) || !rows_of(y, fp8 ? at::kFloat8_e4m3fn : at::kBFloat16, T, d, dev) ||
+      (res && !rows_of(res, at::kBFloat16, T, d, dev)) || (ro && !rows_of(ro, at::kBFloat16, T, d, dev)) ||
+      fp8 != (ys != nullptr) || (ys && !vector_of(ys, at::kFloat, T, dev)))
+    return none();
+  const int64_t ldx = row_stride(x), ldr = row_stride(res), ldo = row_stride(ro), ldy = row_stride(y);
+  const uint16_t *xp = u16(x), *rp = u16(res), *wp = u16(w);
+  uint16_t* op = u16m(ro);
+  void* yp = y->data_ptr();
+  float* sp = ys == nullptr ? nullptr : static_cast<float*>(ys->data_ptr());
+  prc_status st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = fp8 ? reinterpret_cast<decltype(&add_rms_norm_fp8)>(fn)(xp, T, d, ldx, rp, ldr, wp, (float)eps, op, ldo,
+                                                               static_cast<uint8_t*>(yp), ldy, sp, stream)
+           : reinterpret_cast<decltype(&add_rms_norm)>(fn)(xp, T, d, ldx, rp, ldr, wp, (float)eps, op, ldo,
+                                                           static_cast<uint16_t*>(yp), ldy, stream);
+  Py_END_ALLOW_THREADS;
+  return PyLong_FromLong((long)st);
+}
+
+// adapted(fn, size_fn, fp8, X, x_scale, W, w_scale, A, B, agent, Y, workspace, device, stream)
+PyObject* adapted(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 14) return none();
+  void *fn, *size_fn, *stream;
+  const bool fp8 = a[2] == Py_True;
+  const Tensor *X = tensor(a[3]), *W = tensor(a[5]), *Y = tensor(a[10]), *xs, *wsc, *A, *B, *ag, *ws;
+  int64_t dev;
+  if (!as_ptr(a[0], &fn) || !as_ptr(a[1], &size_fn) || !as_ptr(a[13], &stream) || !X || !W || !Y || !opt(a[4], &xs) ||
+      !opt(a[6], &wsc) || !opt(a[7], &A) || !opt(a[8], &B) || !opt(a[9], &ag) || !opt(a[11], &ws) || !as_int(a[12], &dev))
+    return none();
+  if (X->dim() != 2 || W->dim() != 2) return none();
+  const int64_t T = X->size(0), d_in = X->size(1), d_out = W->size(1);
+  const at::ScalarType type = fp8 ? at::kFloat8_e4m3fn : at::kBFloat16;
+  if (!rows_of(X, type, T, d_in, dev) || !rows_of(W, type, d_in, d_out, dev) || !W->is_contiguous() ||
+      !rows_of(Y, at::kBFloat16, T, d_out, dev) || fp8 != (xs != nullptr) || fp8 != (wsc != nullptr) ||
+      (xs && !vector_of(xs, at::kFloat, T, dev)) || (wsc && !vector_of(wsc, at::kFloat, d_out, dev)))
+    return none();
+  int64_t N = 0, r = 0;
+  if ((A != nullptr) != (B != nullptr) || (A != nullptr) != (ag != nullptr)) return none();
+  if (B != nullptr) {
+    if (B->scalar_type() != at::kBFloat16 || B->dim() != 3 || !B->is_contiguous() || B->get_device() != dev) return none();
+    N = B->size(0);
+    r = B->size(1);
+    if (B->size(2) != d_out || !fits({N, r}) || !rows_of(A, at::kBFloat16, d_in, N * r, dev) || !A->is_contiguous() ||
+        !vector_of(ag, at::kInt, T, dev))
+      return none();
+  }
+  if (ws != nullptr && (!ws->is_contiguous() || ws->get_device() != dev)) return none();
+  const size_t need = reinterpret_cast<decltype(&adapted_projection_workspace_size)>(size_fn)(T, d_in, d_out, (int32_t)N, (int32_t)r);
+  if (need > 0 && (ws == nullptr || nbytes(ws) < need)) return need_bytes(need);
+  void* wp = ws == nullptr ? nullptr : ws->data_ptr();
+  const size_t wb = ws == nullptr ? 0 : nbytes(ws);
+  const void *xp = X->data_ptr(), *Wp = W->data_ptr();
+  const float *xsp = xs == nullptr ? nullptr : static_cast<const float*>(xs->data_ptr());
+  const float *wsp = wsc == nullptr ? nullptr : static_cast<const float*>(wsc->data_ptr());
+  const uint16_t *ap = u16(A), *bp = u16(B);
+  const int32_t* gp = i32p(ag);
+  uint16_t* yp = u16m(Y);
+  const int64_t ldx = row_stride(X), ldy = row_stride(Y);
+  prc_status st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = fp8 ? reinterpret_cast<decltype(&adapted_projection_fp8)>(fn)(static_cast<const uint8_t*>(xp), xsp, T, d_in, ldx,
+                                                                     static_cast<const uint8_t*>(Wp), wsp, d_out, ap, bp,
+                                                                     (int32_t)N, (int32_t)r, gp, yp, ldy, wp, wb, stream)
+           : reinterpret_cast<decltype(&adapted_projection)>(fn)(static_cast<const uint16_t*>(xp), T, d_in, ldx,
+                                                                 static_cast<const uint16_t*>(Wp), d_out, ap, bp, (int32_t)N,
+                                                                 (int32_t)r, gp, yp, ldy, wp, wb, stream);
+  Py_END_ALLOW_THREADS;
+  return PyLong_FromLong((long)st);
+}
+
 // A tensor can refuse what is asked of it by throwing (a nested one has no
 // sizes or strides), and nothing may throw through a C entry: such a call is
 // left to Python like any other that is not plain.  (The ABI calls themselves
@@ -359,6 +453,8 @@ PyMethodDef methods[] = {
     method<paged>("paged"),
     method<project>("project"),
     method<project_paged>("project_paged"),
+    method<norm>("norm"),
+    method<adapted>("adapted"),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
