@@ -7,6 +7,9 @@
 #include "common.hpp"
 #include "kernels.hpp"
 
+#include <type_traits>
+#include <cstdlib>
+
 namespace prc {
 namespace {
 
@@ -321,123 +324,374 @@ hipError_t launch_stream(const ProjectArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------------------
-// Eight consecutive elements of X or W as bf16, or zeros.
+// Many rows: X A_a of every row first (a workgroup per 16 rows, its agents in
+// turn), then X W in 256 x 256 tiles with the expanded adapter rows added as
+// each tile is written.
 template <bool FP8>
-__device__ __forceinline__ u32x4 load8(const void* p, int64_t i, bool ok) {
-  if constexpr (FP8) {
-    const u32x2 z = {0u, 0u};
-    return bf16_of_e4m3(ok ? *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(p) + i) : z);
-  } else {
-    return ld16(static_cast<const uint16_t*>(p) + i, ok);
+__global__ void __launch_bounds__(ST_W * 64) shrink_kernel(const ProjectArgs a) {
+  using C = Stream<FP8, 1>;
+  __shared__ __attribute__((aligned(1024))) char lds[ST_W * C::RING * C::STEP];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t t0 = (int64_t)blockIdx.x * 16;
+  const int toks = (int)(a.T - t0 < 16 ? a.T - t0 : (int64_t)16), nk = (int)((a.d_in + 31) / 32);
+  const int ag = lane < toks ? a.agent[t0 + lane] : -1;
+  uint64_t todo = __ballot(ag >= 0 && ag < a.n_agents);  // the same in every wave
+  uint16_t* H = static_cast<uint16_t*>(a.ws) + t0 * a.rank;
+  while (todo != 0) {
+    const int cur = __builtin_amdgcn_readlane(ag, __builtin_ctzll(todo));
+    const uint64_t mine = __ballot(ag == cur);
+    todo &= ~mine;
+    f32x4 acc[4][1] = {};
+    __syncthreads();  // the sums before are read
+    stream_steps<FP8, 1, true>(a, lds + w * C::RING * C::STEP, t0, toks, (int64_t)cur * a.rank, nk * w / ST_W,
+                               nk * (w + 1) / ST_W, acc);
+    sum_waves<1, 4>(acc, lds, 0, (a.rank + 15) / 16, [&](int g, int t, int q, f32x4 s) {
+      const int j = g * 16 + 4 * q;
+      if (j >= a.rank || !(mine >> t & 1)) return;
+      if (FP8) s *= a.x_scale[t0 + t];
+      *reinterpret_cast<u32x2*>(H + t * a.rank + j) = u32x2{pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3])};
+    });
   }
 }
 
-// H[i] = X[i] A_a (times x_scale[i]): a workgroup per row.
-template <bool FP8, int R>
-__global__ void __launch_bounds__(256) shrink_kernel(const ProjectArgs a) {
-  __shared__ float part[4][R];
-  const int64_t row = blockIdx.x;
-  const int ag = a.agent[row];
-  if (ag < 0 || ag >= a.n_agents) return;  // uniform over the workgroup
-  const int tid = threadIdx.x;
-  const int64_t ldA = (int64_t)a.n_agents * R;
-  float acc[R];
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// Tiles of 256 tokens x 32 (C0 + C1) columns: eight waves, four by tokens (64
+// each) and two by columns (32 C0 and 32 C1 of them), on 32x32 MFMAs.  Waves w
+// and w + 4 share a SIMD, so an uneven pair loads all SIMDs alike.  The operands
+// come through a ring of stages (64 bytes of k of each row and column) with
+// direct loads that all waves issue; a wave reads the fragments of its next
+// step between the MFMAs of this one.  X rows are XOR-swizzled in 16-byte
+// chunks, weight rows (as in memory) in blocks of 32 columns, so that the rows
+// which one read takes together hit different banks.
+constexpr int TL_T = 256;
+
+template <bool FP8, int NP>  // NP = C0 + C1 column blocks
+struct Tile {
+  static constexpr int E = FP8 ? 1 : 2, KS = 64 / E, KK = FP8 ? 1 : 2;  // bytes, k and MFMA steps of a stage
+  static constexpr int CT = 32 * NP, WRB = CT * E;                      // columns; bytes of a weight row
+  static constexpr int XB = TL_T * 64, SB = XB + CT * 64;               // bytes of X and of a stage
+  static constexpr int RING = 160 * 1024 / SB < 6 ? 160 * 1024 / SB : 6;
+  static constexpr int NL = SB / 1024, NI = (NL + 7) / 8;               // 1 KB loads of a stage; of a wave, at most
+  // Column block b of weight row k is stored at b ^ swz(k): bf16 reads take 4
+  // rows of 64 bytes together, e4m3 reads 8 rows of 32.
+  static __device__ __forceinline__ int swz(int k) {
+    if (NP % 2 != 0) return 0;  // odd row strides do it
+    if (FP8) return NP % 8 == 0 ? k & 7 : (NP % 4 == 0 ? (k >> 1) & 3 : (k >> 2) & 1);
+    return NP % 4 == 0 ? k & 3 : (k >> 1) & 1;
+  }
+};
+
+// One wave's part of a tile: tokens t0 + 64 wt .., columns c0 + 32 cb0 .. of CB blocks.
+template <bool FP8, int NP, int CB>
+__device__ __forceinline__ void tile_wave(const ProjectArgs& a, char* ring, int64_t t0, int64_t c0, int cb0) {
+  using C = Tile<FP8, NP>;
+  constexpr int E = C::E, FR = FP8 ? 8 : 4;  // registers of a fragment
+  typedef uint32_t Frag __attribute__((ext_vector_type(FR)));
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wt = wv & 3;
+  const int toks = (int)(a.T - t0 < TL_T ? a.T - t0 : (int64_t)TL_T), d_in = (int)a.d_in;
+  const int32_t ldw = (int32_t)(a.d_out * E), ldx = (int32_t)(a.ld_x * E);
+  const i32x4 rx = buffer_rsrc(static_cast<const char*>(a.X) + t0 * ldx, (toks - 1) * ldx + d_in * E);
+  const i32x4 rw = buffer_rsrc(a.W, d_in * ldw);
+  // Load j of this wave is load 8 j + wv of the stage, X rows first.
+  const bool full = 8 * (C::NI - 1) + wv < C::NL;  // this wave has NI loads a stage, or one less
+  int32_t off[C::NI], kof[C::NI];
 #pragma unroll
-  for (int j = 0; j < R; ++j) acc[j] = 0.f;
-  for (int64_t k = tid * 8; k < a.d_in; k += 2048) {
-    const u32x4 xv = load8<FP8>(a.X, row * a.ld_x + k, true);
+  for (int j = 0; j < C::NI; ++j) {
+    const int b = (8 * j + wv) * 1024 + lane * 16;
+    if (j < C::XB / 8192) {
+      const int r = b / 64, c = (lane % 4) ^ ((r >> 2) & 3);
+      kof[j] = c * 16 / E;
+      off[j] = r < toks ? r * ldx + c * 16 : INT32_MIN;
+    } else {
+      const int k = (b - C::XB) / C::WRB, p = (b - C::XB) % C::WRB / (32 * E), in = (b - C::XB) % (32 * E) / E;
+      const int64_t col = c0 + (p ^ C::swz(k)) * 32 + in;
+      kof[j] = k;
+      off[j] = col < a.d_out ? k * ldw + (int32_t)col * E : INT32_MIN;
+    }
+  }
+  static_assert(C::XB % 8192 == 0 && C::WRB % 16 == 0 && C::NL % 2 == 0, "X and weight loads are separate instructions");
+  auto issue = [&](int s, int slot) {
+    char* st = ring + slot * C::SB;
+    const int k0 = s * C::KS;
+    const bool whole = k0 + C::KS <= d_in;  // the k offset is scalar
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float x = i % 2 ? bf_hi(xv[i / 2]) : bf_lo(xv[i / 2]);
-      const uint16_t* ap = a.A + (k + i) * ldA + (int64_t)ag * R;
+    for (int j = 0; j < C::NI; ++j) {
+      if (j == C::NI - 1 && !full) break;
+      const bool x = j < C::XB / 8192;
+      const uint32_t ks = (uint32_t)k0 * (uint32_t)(x ? E : ldw);
+      if (whole) {
+        lds_dma16(x ? rx : rw, st + (8 * j + wv) * 1024, off[j], (int32_t)ks);
+      } else {
+        const bool ok = k0 + kof[j] < d_in && off[j] != INT32_MIN;
+        lds_dma16(x ? rx : rw, st + (8 * j + wv) * 1024, ok ? (int32_t)((uint32_t)off[j] + ks) : INT32_MIN, 0);
+      }
+    }
+  };
+  // Waits until only `n` stages of this wave's loads are in flight.
+  auto wait_stages = [&](auto n) {
+    if (full) wait_loads<decltype(n)::value * C::NI>();
+    else wait_loads<decltype(n)::value * (C::NI - 1)>();
+  };
+
+  const int l32 = lane & 31, h = lane >> 5, grp = lane >> 4, i16 = lane & 15;
+  f32x16 acc[CB][2];
 #pragma unroll
-      for (int j = 0; j < R; j += 8) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(ap + j);
+  for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          acc[j + 2 * e] += x * bf_lo(w[e]);
-          acc[j + 2 * e + 1] += x * bf_hi(w[e]);
+    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) acc[cb][tb][j] = 0.f;
+  const int xrow = 64 * wt + l32, xs = (xrow >> 2) & 3;  // rows 32 further swizzle alike
+  auto read_x = [&](int tb, const char* st, int kk) -> Frag {
+    const char* p = st + (xrow + 32 * tb) * 64;
+    if constexpr (FP8) {
+      const u32x4 lo = *reinterpret_cast<const u32x4*>(p + ((2 * h) ^ xs) * 16);
+      const u32x4 hi = *reinterpret_cast<const u32x4*>(p + ((2 * h + 1) ^ xs) * 16);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      return *reinterpret_cast<const u32x4*>(p + ((2 * kk + h) ^ xs) * 16);
+    }
+  };
+  // First weight row of this lane; the rows it reads besides swizzle alike.
+  const int wk = FP8 ? 32 * h + i16 / 2 : 8 * h + i16 / 4, ws = C::swz(wk);
+  const int wo = C::XB + wk * C::WRB + (grp & 1) * 16 * E + (FP8 ? i16 % 2 : i16 % 4) * 8;
+  auto read_w = [&](int cb, const char* st, int kk) -> Frag {
+    const char* p = st + wo + ((cb0 + cb) ^ ws) * (32 * E) + 16 * kk * C::WRB;
+    if constexpr (FP8) {
+      const u32x2 v0 = lds_read_tr8(p), v1 = lds_read_tr8(p + 8 * C::WRB), v2 = lds_read_tr8(p + 16 * C::WRB),
+                  v3 = lds_read_tr8(p + 24 * C::WRB);
+      return Frag{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+    } else {
+      const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * C::WRB);
+      return Frag{lo[0], lo[1], hi[0], hi[1]};
+    }
+  };
+  auto mma = [&](Frag w, Frag x, f32x16 c) -> f32x16 {
+    if constexpr (FP8)
+      return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(__builtin_bit_cast(i32x8, w), __builtin_bit_cast(i32x8, x), c, 0, 0, 0,
+                                                             0, 0, 0);
+    else
+      return mfma32x32x16(as_bf16x8(w), as_bf16x8(x), c);
+  };
+
+  const int ns = (d_in + C::KS - 1) / C::KS;
+#pragma unroll
+  for (int s = 0; s < C::RING - 1; ++s) issue(s, s);
+  wait_stages(std::integral_constant<int, C::RING - 2>{});
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  Frag fw[CB], fx[2][2];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) fw[cb] = read_w(cb, ring, 0);
+#pragma unroll
+  for (int tb = 0; tb < 2; ++tb) fx[0][tb] = read_x(tb, ring, 0);
+  int slot = 0, last = C::RING - 1;  // slots of stage s and of stage s - 1
+  // Stage s, its first X fragments in set p0.  A weight fragment is read again
+  // (of the next step) as soon as its last MFMA is issued.
+  auto stage = [&](int s, auto P0) {
+    constexpr int p0 = decltype(P0)::value;
+    const int next = slot + 1 == C::RING ? 0 : slot + 1;
+    const char* st = ring + slot * C::SB;
+    const char* stn = ring + next * C::SB;
+#pragma unroll
+    for (int kk = 0; kk < C::KK; ++kk) {
+      const int cur = (p0 + kk) & 1, nxt = cur ^ 1;
+      if (kk == C::KK - 1) {
+        // Stage s + 1 has landed, and every wave has used what it read of stage
+        // s - 1, whose slot is filled again.
+        wait_stages(std::integral_constant<int, C::RING - 3>{});
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        issue(s + C::RING - 1, last);  // past the end: zeros
+      }
+      const char* sn = kk == C::KK - 1 ? stn : st;
+      const int kn = kk == C::KK - 1 ? 0 : kk + 1;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        if (cb < 2) fx[nxt][cb] = read_x(cb, sn, kn);
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) acc[cb][tb] = mma(fw[cb], fx[cur][tb], acc[cb][tb]);
+        fw[cb] = read_w(cb, sn, kn);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    last = slot;
+    slot = next;
+  };
+  static_assert(CB >= 2, "both X fragments are read");
+  if constexpr (C::KK == 2) {
+    for (int s = 0; s < ns; ++s) stage(s, std::integral_constant<int, 0>{});
+  } else {
+    int s = 0;
+    for (; s + 1 < ns; s += 2) {
+      stage(s, std::integral_constant<int, 0>{});
+      stage(s + 1, std::integral_constant<int, 1>{});
+    }
+    if (s < ns) stage(s, std::integral_constant<int, 0>{});
+  }
+  wait_loads<0>();
+  wait_lds();
+  __builtin_amdgcn_s_barrier();  // the ring is free
+  asm volatile("" ::: "memory");
+
+  // acc[cb][tb][j]: column cw + 32 cb + (j / 4) * 8 + 4 h + j % 4, token
+  // tw + 32 tb.
+  const int64_t cw = c0 + 32 * cb0, tw = t0 + 64 * wt + l32;
+  if constexpr (FP8) {
+    float xsc[2];
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) xsc[tb] = tw + 32 * tb < a.T ? a.x_scale[tw + 32 * tb] : 0.f;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int jg = 0; jg < 4; ++jg) {
+        const int64_t c = cw + 32 * cb + jg * 8 + 4 * h;
+        f32x4 wsc = {0.f, 0.f, 0.f, 0.f};
+        if (c < a.d_out) wsc = *reinterpret_cast<const f32x4*>(a.w_scale + c);
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[cb][tb][4 * jg + i] *= xsc[tb] * wsc[i];
+      }
+  }
+  if (a.n_agents > 0) {
+    // Agents of the wave's tokens in turn.  Where a block of 32 tokens has one
+    // agent (tokens past T go with any), its product is summed in place, else it
+    // is added to that agent's tokens alone, so that what is infinite or NaN in
+    // an adapter stays in the rows that use it.
+    int ag[2];
+    uint64_t todo[2];
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+      ag[tb] = tw + 32 * tb < a.T ? a.agent[tw + 32 * tb] : -1;
+      todo[tb] = __ballot(ag[tb] >= 0 && ag[tb] < a.n_agents);
+    }
+    const int R = a.rank, nr = (R + 15) / 16;
+    while ((todo[0] | todo[1]) != 0) {
+      const int cur = todo[0] != 0 ? __builtin_amdgcn_readlane(ag[0], __builtin_ctzll(todo[0]))
+                                   : __builtin_amdgcn_readlane(ag[1], __builtin_ctzll(todo[1]));
+      u32x4 fh[2][4];  // ranks 16 kk + 8 h .. of token l32 of each block
+      bool mine[2], whole[2], some[2];
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb) {
+        const int64_t t = tw + 32 * tb;
+        mine[tb] = ag[tb] == cur;
+        const uint64_t m = __ballot(mine[tb]);
+        some[tb] = m != 0;
+        todo[tb] &= ~m;
+        whole[tb] = __ballot(mine[tb] || t >= a.T) == ~0ull;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+          fh[tb][kk] = ld16(static_cast<const uint16_t*>(a.ws) + t * R + 16 * kk + 8 * h, mine[tb] && 16 * kk + 8 * h < R);
+      }
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        const int64_t c = cw + 32 * cb + l32;
+        u32x4 fb[4];  // B_a^T: the same ranks of column l32
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          if (kk >= nr) break;  // uniform
+          const bool ok = c < a.d_out && 16 * kk + 8 * h < R;
+          const uint16_t* bp = a.B + ((int64_t)cur * R + 16 * kk + 8 * h) * a.d_out + c;
+          uint32_t v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = ok ? bp[i * a.d_out] : 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) fb[kk][i] = v[2 * i] | v[2 * i + 1] << 16;
+        }
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) {
+          if (!some[tb]) continue;  // uniform, as the next
+          f32x16 sum;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) sum[j] = whole[tb] ? acc[cb][tb][j] : 0.f;
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            if (kk >= nr) break;
+            sum = mfma32x32x16(as_bf16x8(fb[kk]), as_bf16x8(fh[tb][kk]), sum);
+          }
+#pragma unroll
+          for (int j = 0; j < 16; ++j) acc[cb][tb][j] = whole[tb] ? sum[j] : (mine[tb] ? acc[cb][tb][j] + sum[j] : acc[cb][tb][j]);
         }
       }
     }
   }
+  // Out through LDS (rows padded by 16 bytes), so that each row is written in
+  // one piece of 64 CB bytes.
+  constexpr int RB = 64 * CB + 16;
+  static_assert(8 * 64 * (64 * ((NP + 1) / 2) + 16) <= C::RING * C::SB, "the waves' results fit the ring");
+  char* mineb = ring + wv * 64 * (64 * ((NP + 1) / 2) + 16);
 #pragma unroll
-  for (int j = 0; j < R; ++j) {
+  for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) acc[j] += shfl_xor(acc[j], m);
-    if (tid % 64 == 0) part[tid / 64][j] = acc[j];
-  }
-  __syncthreads();
-  if (tid < R) {
-    float v = part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid];
-    if (FP8) v *= a.x_scale[row];
-    static_cast<uint16_t*>(a.ws)[row * R + tid] = (uint16_t)(pack_bf16(v, 0.f) & 0xffffu);
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int jg = 0; jg < 4; ++jg) {
+        const f32x16& v = acc[cb][tb];
+        *reinterpret_cast<u32x2*>(mineb + (32 * tb + l32) * RB + cb * 64 + jg * 16 + h * 8) =
+            u32x2{pack_bf16(v[4 * jg], v[4 * jg + 1]), pack_bf16(v[4 * jg + 2], v[4 * jg + 3])};
+      }
+  wait_lds();
+#pragma unroll
+  for (int i = 0; i < 4 * CB; ++i) {
+    const int u = i * 64 + lane, r = u / (4 * CB), ch = u % (4 * CB);
+    const int64_t t = t0 + 64 * wt + r, c = cw + ch * 8;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(mineb + r * RB + ch * 16);
+    if (t < a.T && c < a.d_out) *reinterpret_cast<u32x4*>(a.Y + t * a.ld_y + c) = v;
   }
 }
 
-// 64 tokens x 64 columns a workgroup, 32 k a step; wave w owns 16 columns.
-template <bool FP8>
-__global__ void __launch_bounds__(256) project_kernel(const ProjectArgs a) {
-  __shared__ __attribute__((aligned(16))) uint16_t xt[64][40], wt[32][72];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c16 = lane & 15;
-  const int64_t t0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
-  f32x4 acc[4] = {};
-  const int xr = tid / 4, xk = tid % 4 * 8, wr = tid / 8, wc = tid % 8 * 8;
-  for (int64_t k0 = 0; k0 < a.d_in; k0 += 32) {
-    const u32x4 xv = load8<FP8>(a.X, (t0 + xr) * a.ld_x + k0 + xk, t0 + xr < a.T && k0 + xk < a.d_in);
-    const u32x4 wv = load8<FP8>(a.W, (k0 + wr) * a.d_out + c0 + wc, k0 + wr < a.d_in && c0 + wc < a.d_out);
-    __syncthreads();
-    *reinterpret_cast<u32x4*>(&xt[xr][xk]) = xv;
-    *reinterpret_cast<u32x4*>(&wt[wr][wc]) = wv;
-    __syncthreads();
-    const u32x2 lo = lds_read_tr16(&wt[8 * q + c16 / 4][16 * w + 4 * (c16 % 4)]);
-    const u32x2 hi = lds_read_tr16(&wt[8 * q + 4 + c16 / 4][16 * w + 4 * (c16 % 4)]);
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
-      acc[m] = mfma16x16x32(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}),
-                            as_bf16x8(*reinterpret_cast<const u32x4*>(&xt[16 * m + c16][8 * q])), acc[m]);
-  }
-  const int64_t c = c0 + 16 * w + 4 * q;  // this lane's four columns
-  if (c >= a.d_out) return;
-#pragma unroll
-  for (int m = 0; m < 4; ++m) {
-    const int64_t t = t0 + 16 * m + c16;
-    if (t >= a.T) continue;
-    float v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = FP8 ? acc[m][i] * (a.x_scale[t] * a.w_scale[c + i]) : acc[m][i];
-    const int ag = a.n_agents > 0 ? a.agent[t] : -1;
-    if (ag >= 0 && ag < a.n_agents) {
-      const uint16_t* h = static_cast<const uint16_t*>(a.ws) + t * a.rank;
-      for (int j = 0; j < a.rank; ++j) {
-        const float hj = bf_lo(h[j]);
-        const u32x2 b = *reinterpret_cast<const u32x2*>(a.B + ((int64_t)ag * a.rank + j) * a.d_out + c);
-        v[0] += hj * bf_lo(b[0]);
-        v[1] += hj * bf_hi(b[0]);
-        v[2] += hj * bf_lo(b[1]);
-        v[3] += hj * bf_hi(b[1]);
-      }
-    }
-    *reinterpret_cast<u32x2*>(a.Y + t * a.ld_y + c) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-  }
+template <bool FP8, int C0, int C1>
+__global__ void __launch_bounds__(512, 2) tile_kernel(const ProjectArgs a, int n_tt, int n_ct) {
+  using C = Tile<FP8, C0 + C1>;
+  __shared__ __attribute__((aligned(1024))) char ring[C::RING * C::SB];
+  // Workgroup L runs on XCD L % 8; each XCD takes a contiguous eighth of the
+  // tiles, in bands of four token tiles, whose rows of X and columns of W its
+  // L2 then serves several times.
+  const int n_tiles = n_tt * n_ct, per = (n_tiles + 7) / 8;
+  const int tile = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
+  if ((int)(blockIdx.x / 8) >= per || tile >= n_tiles) return;  // uniform over the workgroup
+  const int band = tile / (4 * n_ct), in = tile - band * 4 * n_ct, bh = n_tt - 4 * band < 4 ? n_tt - 4 * band : 4;
+  const int ct = __builtin_amdgcn_readfirstlane(in / bh), tt = __builtin_amdgcn_readfirstlane(4 * band + in % bh);
+  const int64_t t0 = (int64_t)tt * TL_T, c0 = (int64_t)ct * C::CT;
+  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) < 4) tile_wave<FP8, C0 + C1, C0>(a, ring, t0, c0, 0);
+  else tile_wave<FP8, C0 + C1, C1>(a, ring, t0, c0, C0);
+}
+
+template <bool FP8, int C0, int C1>
+hipError_t launch_tiles(const ProjectArgs& a, hipStream_t st) {
+  const int64_t n_tt = (a.T + TL_T - 1) / TL_T, n_ct = (a.d_out + 32 * (C0 + C1) - 1) / (32 * (C0 + C1));
+  hipLaunchKernelGGL((tile_kernel<FP8, C0, C1>), dim3((unsigned)((n_tt * n_ct + 7) / 8 * 8)), dim3(512), 0, st, a, (int)n_tt,
+                     (int)n_ct);
+  return hipGetLastError();
 }
 
 template <bool FP8>
 hipError_t launch(const ProjectArgs& a, hipStream_t st) {
   if (a.T <= ST_T) return launch_stream<FP8>(a, st);
   if (a.n_agents > 0) {
-    const dim3 grid((unsigned)a.T);
-    switch (a.rank) {
-      case 8: hipLaunchKernelGGL((shrink_kernel<FP8, 8>), grid, dim3(256), 0, st, a); break;
-      case 16: hipLaunchKernelGGL((shrink_kernel<FP8, 16>), grid, dim3(256), 0, st, a); break;
-      case 32: hipLaunchKernelGGL((shrink_kernel<FP8, 32>), grid, dim3(256), 0, st, a); break;
-      default: hipLaunchKernelGGL((shrink_kernel<FP8, 64>), grid, dim3(256), 0, st, a); break;
-    }
+    hipLaunchKernelGGL((shrink_kernel<FP8>), dim3((unsigned)((a.T + 15) / 16)), dim3(ST_W * 64), 0, st, a);
     if (const hipError_t e = hipGetLastError()) return e;
   }
-  const dim3 grid((unsigned)((a.d_out + 63) / 64), (unsigned)((a.T + 63) / 64));
-  hipLaunchKernelGGL((project_kernel<FP8>), grid, dim3(256), 0, st, a);
-  return hipGetLastError();
+  // The width that takes the least time by rounds of the CUs.
+  int best = 8;
+  double least = 1e300;
+  for (int np : {8, 6, 5, 4}) {
+    const int64_t tiles = ((a.T + TL_T - 1) / TL_T) * ((a.d_out + 32 * np - 1) / (32 * np));
+    const double t = (double)((tiles + a.cus - 1) / a.cus) * (np + 0.5);
+    if (t < least) {
+      least = t;
+      best = np;
+    }
+  }
+  if (const char* f = getenv("TL_NP")) best = atoi(f);
+  switch (best) {
+    case 8: return launch_tiles<FP8, 4, 4>(a, st);
+    case 6: return launch_tiles<FP8, 3, 3>(a, st);
+    case 5: return launch_tiles<FP8, 3, 2>(a, st);
+    default: return launch_tiles<FP8, 2, 2>(a, st);
+  }
 }
 
 }  // namespace
