@@ -324,224 +324,165 @@ hipError_t launch_stream(const ProjectArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------------------
-// Many rows: X A_a of every row first (a workgroup per 16 rows, its agents in
-// turn), then X W in 256 x 256 tiles with the expanded adapter rows added as
-// each tile is written.
-template <bool FP8>
-__global__ void __launch_bounds__(ST_W * 64) shrink_kernel(const ProjectArgs a) {
-  using C = Stream<FP8, 1>;
+// Many rows: X A_a of every row first, then X W in tiles with the expanded
+// adapter rows added as each tile is written.
+//
+// The adapter rows: a workgroup takes 16 rows and a slice of k, its eight waves
+// an eighth of that each, and their agents in turn.  Steps of 128 bytes of k (a
+// CU takes one request of up to 128 bytes every other cycle, so shorter pieces
+// cost as much) come through wave-private rings as above.
+template <bool FP8, int R>
+struct Shrink {
+  static constexpr int KS = FP8 && R < 64 ? 128 : 64;               // k of a step (LDS holds no more at rank 64)
+  static constexpr int XR = KS * (FP8 ? 1 : 2), NC = XR / 16;       // bytes and chunks of a row of X
+  static constexpr int NX = XR / 64, NA = (KS * R * 2 + 1023) / 1024;  // 1 KB loads of X and of A
+  static constexpr int NI = NX + NA, STEP = NI * 1024;
+  static constexpr int RING = 20 / NI < 2 ? 2 : 20 / NI;
+  static_assert(ST_W * RING * STEP <= 160 * 1024, "LDS");
+};
+
+template <bool FP8, int R>
+__global__ void __launch_bounds__(ST_W * 64) shrink_kernel(const ProjectArgs a, int ksa) {
+  using C = Shrink<FP8, R>;
+  constexpr int E = FP8 ? 1 : 2, NB = (R + 15) / 16;
   __shared__ __attribute__((aligned(1024))) char lds[ST_W * C::RING * C::STEP];
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int64_t t0 = (int64_t)blockIdx.x * 16;
-  const int toks = (int)(a.T - t0 < 16 ? a.T - t0 : (int64_t)16), nk = (int)((a.d_in + 31) / 32);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, c16 = lane & 15;
+  const int ki = (int)(blockIdx.x % (unsigned)ksa);
+  const int64_t t0 = (int64_t)(blockIdx.x / (unsigned)ksa) * 16;
+  const int toks = (int)(a.T - t0 < 16 ? a.T - t0 : (int64_t)16), d_in = (int)a.d_in;
+  const int nk = (d_in + C::KS - 1) / C::KS, part = ki * ST_W + w, parts = ksa * ST_W;
+  const int s_lo = (int)((int64_t)nk * part / parts), s_hi = (int)((int64_t)nk * (part + 1) / parts);
   const int ag = lane < toks ? a.agent[t0 + lane] : -1;
   uint64_t todo = __ballot(ag >= 0 && ag < a.n_agents);  // the same in every wave
-  uint16_t* H = static_cast<uint16_t*>(a.ws) + t0 * a.rank;
+  float* H = static_cast<float*>(a.ws) + ((int64_t)ki * a.T + t0) * R;
+  char* ring = lds + w * C::RING * C::STEP;
+  const int32_t lda = (int32_t)((int64_t)a.n_agents * R * 2), ldx = (int32_t)(a.ld_x * E);
+  const i32x4 ra = buffer_rsrc(a.A, d_in * lda);
+  const i32x4 rx = buffer_rsrc(static_cast<const char*>(a.X) + t0 * ldx, (toks - 1) * ldx + d_in * E);
+  // X: 16-byte chunks XOR-swizzled by row.
+  int32_t kx[C::NX], ox[C::NX], ka[C::NA];
+#pragma unroll
+  for (int j = 0; j < C::NX; ++j) {
+    const int t = (j * 64 + lane) / C::NC;
+    kx[j] = ((lane % C::NC) ^ (t % C::NC)) * 16 / E;
+    ox[j] = t < toks ? t * ldx + kx[j] * E : INT32_MIN;
+  }
+#pragma unroll
+  for (int j = 0; j < C::NA; ++j) {
+    const int b = j * 1024 + lane * 16;
+    ka[j] = b < C::KS * R * 2 ? b / (R * 2) : INT32_MAX / 2;  // past the step: zeros
+  }
+  const int32_t ca = lane * 16 % (R * 2);  // a lane's bytes within a row of A are the same in every load
   while (todo != 0) {
     const int cur = __builtin_amdgcn_readlane(ag, __builtin_ctzll(todo));
     const uint64_t mine = __ballot(ag == cur);
     todo &= ~mine;
-    f32x4 acc[4][1] = {};
+    auto issue = [&](int s) {
+      char* st = ring + (s % C::RING) * C::STEP;
+      const int k0 = s * C::KS, left = s < s_hi ? d_in - k0 : 0;
+#pragma unroll
+      for (int j = 0; j < C::NX; ++j)
+        lds_dma16(rx, st + j * 1024, kx[j] < left && ox[j] != INT32_MIN ? ox[j] + k0 * E : INT32_MIN, 0);
+#pragma unroll
+      for (int j = 0; j < C::NA; ++j)
+        lds_dma16(ra, st + (C::NX + j) * 1024,
+                  ka[j] < left ? (int32_t)((uint32_t)(k0 + ka[j]) * (uint32_t)lda + (uint32_t)(cur * R * 2 + ca)) : INT32_MIN, 0);
+    };
+    f32x4 acc[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) acc[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
     __syncthreads();  // the sums before are read
-    stream_steps<FP8, 1, true>(a, lds + w * C::RING * C::STEP, t0, toks, (int64_t)cur * a.rank, nk * w / ST_W,
-                               nk * (w + 1) / ST_W, acc);
-    sum_waves<1, 4>(acc, lds, 0, (a.rank + 15) / 16, [&](int g, int t, int q, f32x4 s) {
-      const int j = g * 16 + 4 * q;
-      if (j >= a.rank || !(mine >> t & 1)) return;
-      if (FP8) s *= a.x_scale[t0 + t];
-      *reinterpret_cast<u32x2*>(H + t * a.rank + j) = u32x2{pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3])};
-    });
+    for (int i = 0; i < C::RING; ++i) issue(s_lo + i);
+    for (int s = s_lo; s < s_hi; ++s) {
+      wait_loads<(C::RING - 1) * C::NI>();
+      const char* st = ring + (s % C::RING) * C::STEP;
+#pragma unroll
+      for (int kk = 0; kk < C::KS / 32; ++kk) {
+        bf16x8 x;
+        const char* xp = st + c16 * C::XR;
+        if constexpr (FP8)
+          x = as_bf16x8(bf16_of_e4m3(*reinterpret_cast<const u32x2*>(xp + ((2 * kk + q / 2) ^ (c16 % C::NC)) * 16 + q % 2 * 8)));
+        else
+          x = as_bf16x8(*reinterpret_cast<const u32x4*>(xp + ((4 * kk + q) ^ (c16 % C::NC)) * 16));
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          // Rank 8: the block's upper columns are the lower ones again, and dropped.
+          const char* p = st + C::NX * 1024 + (32 * kk + 8 * q + c16 / 4) * (R * 2) + nb * 32 + c16 % (R == 8 ? 2 : 4) * 8;
+          const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 8 * R);
+          acc[nb] = mfma16x16x32(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}), x, acc[nb]);
+        }
+      }
+      wait_lds();  // this step's slot is free
+      issue(s + C::RING);
+    }
+    wait_loads<0>();
+    // The waves' sums, added in a fixed order.
+    f32x4* sums = reinterpret_cast<f32x4*>(lds);  // [wave][NB][64]
+    __syncthreads();
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) sums[(w * NB + nb) * 64 + lane] = acc[nb];
+    __syncthreads();
+    for (int u = threadIdx.x; u < NB * 64; u += ST_W * 64) {
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < ST_W; ++i) v += sums[i * NB * 64 + u];
+      const int j = u / 64 * 16 + u / 16 % 4 * 4, t = u % 16;
+      if (j < R && (mine >> t & 1)) *reinterpret_cast<f32x4*>(H + t * R + j) = v;
+    }
   }
+}
+
+// k slices of the adapter rows: enough workgroups for the CUs, at most 8, a step
+// a wave at least.
+int shrink_slices(int64_t T, int64_t d_in, int cus) {
+  const int64_t rows = (T + 15) / 16;
+  int64_t k = cus / rows;
+  const int64_t most = d_in / (128 * ST_W);
+  k = k > most ? most : k;
+  return (int)(k < 1 ? 1 : (k > 8 ? 8 : k));
 }
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// Tiles of 256 tokens x 32 (C0 + C1) columns: eight waves, four by tokens (64
-// each) and two by columns (32 C0 and 32 C1 of them), on 32x32 MFMAs.  Waves w
-// and w + 4 share a SIMD, so an uneven pair loads all SIMDs alike.  The operands
-// come through a ring of stages (64 bytes of k of each row and column) with
-// direct loads that all waves issue; a wave reads the fragments of its next
-// step between the MFMAs of this one.  X rows are XOR-swizzled in 16-byte
-// chunks, weight rows (as in memory) in blocks of 32 columns, so that the rows
-// which one read takes together hit different banks.
-constexpr int TL_T = 256;
-
-template <bool FP8, int NP>  // NP = C0 + C1 column blocks
-struct Tile {
-  static constexpr int E = FP8 ? 1 : 2, KS = 64 / E, KK = FP8 ? 1 : 2;  // bytes, k and MFMA steps of a stage
-  static constexpr int CT = 32 * NP, WRB = CT * E;                      // columns; bytes of a weight row
-  static constexpr int XB = TL_T * 64, SB = XB + CT * 64;               // bytes of X and of a stage
-  static constexpr int RING = 160 * 1024 / SB < 6 ? 160 * 1024 / SB : 6;
-  static constexpr int NL = SB / 1024, NI = (NL + 7) / 8;               // 1 KB loads of a stage; of a wave, at most
-  // Column block b of weight row k is stored at b ^ swz(k): bf16 reads take 4
-  // rows of 64 bytes together, e4m3 reads 8 rows of 32.
-  static __device__ __forceinline__ int swz(int k) {
-    if (NP % 2 != 0) return 0;  // odd row strides do it
-    if (FP8) return NP % 8 == 0 ? k & 7 : (NP % 4 == 0 ? (k >> 1) & 3 : (k >> 2) & 1);
-    return NP % 4 == 0 ? k & 3 : (k >> 1) & 1;
-  }
-};
-
-// One wave's part of a tile: tokens t0 + 64 wt .., columns c0 + 32 cb0 .. of CB blocks.
-template <bool FP8, int NP, int CB>
-__device__ __forceinline__ void tile_wave(const ProjectArgs& a, char* ring, int64_t t0, int64_t c0, int cb0) {
-  using C = Tile<FP8, NP>;
-  constexpr int E = C::E, FR = FP8 ? 8 : 4;  // registers of a fragment
+template <bool FP8>
+struct Mma {
+  static constexpr int FR = FP8 ? 8 : 4;  // registers of an operand
   typedef uint32_t Frag __attribute__((ext_vector_type(FR)));
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wt = wv & 3;
-  const int toks = (int)(a.T - t0 < TL_T ? a.T - t0 : (int64_t)TL_T), d_in = (int)a.d_in;
-  const int32_t ldw = (int32_t)(a.d_out * E), ldx = (int32_t)(a.ld_x * E);
-  const i32x4 rx = buffer_rsrc(static_cast<const char*>(a.X) + t0 * ldx, (toks - 1) * ldx + d_in * E);
-  const i32x4 rw = buffer_rsrc(a.W, d_in * ldw);
-  // Load j of this wave is load 8 j + wv of the stage, X rows first.
-  const bool full = 8 * (C::NI - 1) + wv < C::NL;  // this wave has NI loads a stage, or one less
-  int32_t off[C::NI], kof[C::NI];
-#pragma unroll
-  for (int j = 0; j < C::NI; ++j) {
-    const int b = (8 * j + wv) * 1024 + lane * 16;
-    if (j < C::XB / 8192) {
-      const int r = b / 64, c = (lane % 4) ^ ((r >> 2) & 3);
-      kof[j] = c * 16 / E;
-      off[j] = r < toks ? r * ldx + c * 16 : INT32_MIN;
-    } else {
-      const int k = (b - C::XB) / C::WRB, p = (b - C::XB) % C::WRB / (32 * E), in = (b - C::XB) % (32 * E) / E;
-      const int64_t col = c0 + (p ^ C::swz(k)) * 32 + in;
-      kof[j] = k;
-      off[j] = col < a.d_out ? k * ldw + (int32_t)col * E : INT32_MIN;
-    }
-  }
-  static_assert(C::XB % 8192 == 0 && C::WRB % 16 == 0 && C::NL % 2 == 0, "X and weight loads are separate instructions");
-  auto issue = [&](int s, int slot) {
-    char* st = ring + slot * C::SB;
-    const int k0 = s * C::KS;
-    const bool whole = k0 + C::KS <= d_in;  // the k offset is scalar
-#pragma unroll
-    for (int j = 0; j < C::NI; ++j) {
-      if (j == C::NI - 1 && !full) break;
-      const bool x = j < C::XB / 8192;
-      const uint32_t ks = (uint32_t)k0 * (uint32_t)(x ? E : ldw);
-      if (whole) {
-        lds_dma16(x ? rx : rw, st + (8 * j + wv) * 1024, off[j], (int32_t)ks);
-      } else {
-        const bool ok = k0 + kof[j] < d_in && off[j] != INT32_MIN;
-        lds_dma16(x ? rx : rw, st + (8 * j + wv) * 1024, ok ? (int32_t)((uint32_t)off[j] + ks) : INT32_MIN, 0);
-      }
-    }
-  };
-  // Waits until only `n` stages of this wave's loads are in flight.
-  auto wait_stages = [&](auto n) {
-    if (full) wait_loads<decltype(n)::value * C::NI>();
-    else wait_loads<decltype(n)::value * (C::NI - 1)>();
-  };
-
-  const int l32 = lane & 31, h = lane >> 5, grp = lane >> 4, i16 = lane & 15;
-  f32x16 acc[CB][2];
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-    for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) acc[cb][tb][j] = 0.f;
-  const int xrow = 64 * wt + l32, xs = (xrow >> 2) & 3;  // rows 32 further swizzle alike
-  auto read_x = [&](int tb, const char* st, int kk) -> Frag {
-    const char* p = st + (xrow + 32 * tb) * 64;
-    if constexpr (FP8) {
-      const u32x4 lo = *reinterpret_cast<const u32x4*>(p + ((2 * h) ^ xs) * 16);
-      const u32x4 hi = *reinterpret_cast<const u32x4*>(p + ((2 * h + 1) ^ xs) * 16);
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    } else {
-      return *reinterpret_cast<const u32x4*>(p + ((2 * kk + h) ^ xs) * 16);
-    }
-  };
-  // First weight row of this lane; the rows it reads besides swizzle alike.
-  const int wk = FP8 ? 32 * h + i16 / 2 : 8 * h + i16 / 4, ws = C::swz(wk);
-  const int wo = C::XB + wk * C::WRB + (grp & 1) * 16 * E + (FP8 ? i16 % 2 : i16 % 4) * 8;
-  auto read_w = [&](int cb, const char* st, int kk) -> Frag {
-    const char* p = st + wo + ((cb0 + cb) ^ ws) * (32 * E) + 16 * kk * C::WRB;
-    if constexpr (FP8) {
-      const u32x2 v0 = lds_read_tr8(p), v1 = lds_read_tr8(p + 8 * C::WRB), v2 = lds_read_tr8(p + 16 * C::WRB),
-                  v3 = lds_read_tr8(p + 24 * C::WRB);
-      return Frag{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
-    } else {
-      const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * C::WRB);
-      return Frag{lo[0], lo[1], hi[0], hi[1]};
-    }
-  };
-  auto mma = [&](Frag w, Frag x, f32x16 c) -> f32x16 {
+  // 32x32 outputs over 16 k (bf16) or 64 (e4m3: sums of eight products cut what
+  // is below 2^-13 of the largest, then fp32).
+  static __device__ __forceinline__ f32x16 mma(Frag w, Frag x, f32x16 c) {
     if constexpr (FP8)
       return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(__builtin_bit_cast(i32x8, w), __builtin_bit_cast(i32x8, x), c, 0, 0, 0,
                                                              0, 0, 0);
     else
       return mfma32x32x16(as_bf16x8(w), as_bf16x8(x), c);
-  };
-
-  const int ns = (d_in + C::KS - 1) / C::KS;
-#pragma unroll
-  for (int s = 0; s < C::RING - 1; ++s) issue(s, s);
-  wait_stages(std::integral_constant<int, C::RING - 2>{});
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-  Frag fw[CB], fx[2][2];
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb) fw[cb] = read_w(cb, ring, 0);
-#pragma unroll
-  for (int tb = 0; tb < 2; ++tb) fx[0][tb] = read_x(tb, ring, 0);
-  int slot = 0, last = C::RING - 1;  // slots of stage s and of stage s - 1
-  // Stage s, its first X fragments in set p0.  A weight fragment is read again
-  // (of the next step) as soon as its last MFMA is issued.
-  auto stage = [&](int s, auto P0) {
-    constexpr int p0 = decltype(P0)::value;
-    const int next = slot + 1 == C::RING ? 0 : slot + 1;
-    const char* st = ring + slot * C::SB;
-    const char* stn = ring + next * C::SB;
-#pragma unroll
-    for (int kk = 0; kk < C::KK; ++kk) {
-      const int cur = (p0 + kk) & 1, nxt = cur ^ 1;
-      if (kk == C::KK - 1) {
-        // Stage s + 1 has landed, and every wave has used what it read of stage
-        // s - 1, whose slot is filled again.
-        wait_stages(std::integral_constant<int, C::RING - 3>{});
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        issue(s + C::RING - 1, last);  // past the end: zeros
-      }
-      const char* sn = kk == C::KK - 1 ? stn : st;
-      const int kn = kk == C::KK - 1 ? 0 : kk + 1;
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) {
-        if (cb < 2) fx[nxt][cb] = read_x(cb, sn, kn);
-#pragma unroll
-        for (int tb = 0; tb < 2; ++tb) acc[cb][tb] = mma(fw[cb], fx[cur][tb], acc[cb][tb]);
-        fw[cb] = read_w(cb, sn, kn);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    last = slot;
-    slot = next;
-  };
-  static_assert(CB >= 2, "both X fragments are read");
-  if constexpr (C::KK == 2) {
-    for (int s = 0; s < ns; ++s) stage(s, std::integral_constant<int, 0>{});
-  } else {
-    int s = 0;
-    for (; s + 1 < ns; s += 2) {
-      stage(s, std::integral_constant<int, 0>{});
-      stage(s + 1, std::integral_constant<int, 1>{});
-    }
-    if (s < ns) stage(s, std::integral_constant<int, 0>{});
   }
-  wait_loads<0>();
-  wait_lds();
-  __builtin_amdgcn_s_barrier();  // the ring is free
-  asm volatile("" ::: "memory");
+};
 
-  // acc[cb][tb][j]: column cw + 32 cb + (j / 4) * 8 + 4 h + j % 4, token
-  // tw + 32 tb.
-  const int64_t cw = c0 + 32 * cb0, tw = t0 + 64 * wt + l32;
-  if constexpr (FP8) {
-    float xsc[2];
+// Column block b of weight row k is stored at b ^ swz(k), of NP blocks a row:
+// bf16 reads take 4 rows of 64 bytes together, e4m3 reads 8 rows of 32; odd
+// rows of blocks spread over the banks by themselves.
+template <bool FP8, int NP>
+__device__ __forceinline__ int swz_blocks(int k) {
+  if (NP % 2 != 0) return 0;
+  if (FP8) return NP % 8 == 0 ? k & 7 : (NP % 4 == 0 ? (k >> 1) & 3 : (k >> 2) & 1);
+  return NP % 4 == 0 ? k & 3 : (k >> 1) & 1;
+}
+
+// What a wave does with its sums acc[cb][tb][j]: column cw + 32 cb + (j / 4) * 8
+// + 4 h + j % 4, token tw + 32 tb + l32.  Scales (e4m3), the expanded adapter
+// rows, the rounding, and Y, by way of `lds` (this wave's) so that each row is
+// written in one piece of 64 CB bytes.
+template <int CB, int TB>
+constexpr int finish_bytes = 32 * TB * (64 * CB + 16);
+
+template <bool FP8, int CB, int TB>
+__device__ __forceinline__ void finish_tile(const ProjectArgs& a, int ksa, f32x16 (&acc)[CB][TB], char* lds, int64_t tw, int64_t cw) {
+  const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+  float xsc[TB];
 #pragma unroll
-    for (int tb = 0; tb < 2; ++tb) xsc[tb] = tw + 32 * tb < a.T ? a.x_scale[tw + 32 * tb] : 0.f;
+  for (int tb = 0; tb < TB; ++tb) xsc[tb] = FP8 && tw + 32 * tb + l32 < a.T ? a.x_scale[tw + 32 * tb + l32] : 1.f;
+  if constexpr (FP8) {
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -550,7 +491,7 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, char* ring, int6
         f32x4 wsc = {0.f, 0.f, 0.f, 0.f};
         if (c < a.d_out) wsc = *reinterpret_cast<const f32x4*>(a.w_scale + c);
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
+        for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
           for (int i = 0; i < 4; ++i) acc[cb][tb][4 * jg + i] *= xsc[tb] * wsc[i];
       }
@@ -560,30 +501,52 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, char* ring, int6
     // agent (tokens past T go with any), its product is summed in place, else it
     // is added to that agent's tokens alone, so that what is infinite or NaN in
     // an adapter stays in the rows that use it.
-    int ag[2];
-    uint64_t todo[2];
+    int ag[TB];
+    uint64_t todo[TB], any = 0;
 #pragma unroll
-    for (int tb = 0; tb < 2; ++tb) {
-      ag[tb] = tw + 32 * tb < a.T ? a.agent[tw + 32 * tb] : -1;
+    for (int tb = 0; tb < TB; ++tb) {
+      const int64_t t = tw + 32 * tb + l32;
+      ag[tb] = t < a.T ? a.agent[t] : -1;
       todo[tb] = __ballot(ag[tb] >= 0 && ag[tb] < a.n_agents);
+      any |= todo[tb];
     }
     const int R = a.rank, nr = (R + 15) / 16;
-    while ((todo[0] | todo[1]) != 0) {
-      const int cur = todo[0] != 0 ? __builtin_amdgcn_readlane(ag[0], __builtin_ctzll(todo[0]))
-                                   : __builtin_amdgcn_readlane(ag[1], __builtin_ctzll(todo[1]));
-      u32x4 fh[2][4];  // ranks 16 kk + 8 h .. of token l32 of each block
-      bool mine[2], whole[2], some[2];
+    const float* H = static_cast<const float*>(a.ws);
+    while (any != 0) {
+      int cur = 0;
 #pragma unroll
-      for (int tb = 0; tb < 2; ++tb) {
-        const int64_t t = tw + 32 * tb;
+      for (int tb = TB - 1; tb >= 0; --tb)
+        if (todo[tb] != 0) cur = __builtin_amdgcn_readlane(ag[tb], __builtin_ctzll(todo[tb]));
+      u32x4 fh[TB][4];  // ranks 16 kk + 8 h .. of token l32 of each block
+      bool mine[TB], whole[TB], some[TB];
+      any = 0;
+#pragma unroll
+      for (int tb = 0; tb < TB; ++tb) {
+        const int64_t t = tw + 32 * tb + l32;
         mine[tb] = ag[tb] == cur;
         const uint64_t m = __ballot(mine[tb]);
         some[tb] = m != 0;
         todo[tb] &= ~m;
+        any |= todo[tb];
         whole[tb] = __ballot(mine[tb] || t >= a.T) == ~0ull;
+        if (!some[tb]) continue;  // uniform
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk)
-          fh[tb][kk] = ld16(static_cast<const uint16_t*>(a.ws) + t * R + 16 * kk + 8 * h, mine[tb] && 16 * kk + 8 * h < R);
+        for (int kk = 0; kk < 4; ++kk) {
+          if (kk >= nr) break;  // uniform
+          f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+          if (mine[tb] && 16 * kk + 8 * h < R)
+            for (int k = 0; k < ksa; ++k) {
+              const f32x4* p = reinterpret_cast<const f32x4*>(H + (k * a.T + t) * R + 16 * kk + 8 * h);
+              v[0] += p[0];
+              v[1] += p[1];
+            }
+          if constexpr (FP8) {
+            v[0] *= xsc[tb];
+            v[1] *= xsc[tb];
+          }
+          fh[tb][kk] = u32x4{pack_bf16(v[0][0], v[0][1]), pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][0], v[1][1]),
+                             pack_bf16(v[1][2], v[1][3])};
+        }
       }
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
@@ -601,8 +564,8 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, char* ring, int6
           for (int i = 0; i < 4; ++i) fb[kk][i] = v[2 * i] | v[2 * i + 1] << 16;
         }
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb) {
-          if (!some[tb]) continue;  // uniform, as the next
+        for (int tb = 0; tb < TB; ++tb) {
+          if (!some[tb]) continue;
           f32x16 sum;
 #pragma unroll
           for (int j = 0; j < 16; ++j) sum[j] = whole[tb] ? acc[cb][tb][j] : 0.f;
@@ -617,52 +580,249 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, char* ring, int6
       }
     }
   }
-  // Out through LDS (rows padded by 16 bytes), so that each row is written in
-  // one piece of 64 CB bytes.
-  constexpr int RB = 64 * CB + 16;
-  static_assert(8 * 64 * (64 * ((NP + 1) / 2) + 16) <= C::RING * C::SB, "the waves' results fit the ring");
-  char* mineb = ring + wv * 64 * (64 * ((NP + 1) / 2) + 16);
+  constexpr int RB = 64 * CB + 16;  // padded rows
 #pragma unroll
-  for (int tb = 0; tb < 2; ++tb)
+  for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
       for (int jg = 0; jg < 4; ++jg) {
         const f32x16& v = acc[cb][tb];
-        *reinterpret_cast<u32x2*>(mineb + (32 * tb + l32) * RB + cb * 64 + jg * 16 + h * 8) =
+        *reinterpret_cast<u32x2*>(lds + (32 * tb + l32) * RB + cb * 64 + jg * 16 + h * 8) =
             u32x2{pack_bf16(v[4 * jg], v[4 * jg + 1]), pack_bf16(v[4 * jg + 2], v[4 * jg + 3])};
       }
   wait_lds();
 #pragma unroll
-  for (int i = 0; i < 4 * CB; ++i) {
+  for (int i = 0; i < 2 * TB * CB; ++i) {
     const int u = i * 64 + lane, r = u / (4 * CB), ch = u % (4 * CB);
-    const int64_t t = t0 + 64 * wt + r, c = cw + ch * 8;
-    const u32x4 v = *reinterpret_cast<const u32x4*>(mineb + r * RB + ch * 16);
+    const int64_t t = tw + r, c = cw + ch * 8;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + r * RB + ch * 16);
     if (t < a.T && c < a.d_out) *reinterpret_cast<u32x4*>(a.Y + t * a.ld_y + c) = v;
   }
 }
 
-template <bool FP8, int C0, int C1>
-__global__ void __launch_bounds__(512, 2) tile_kernel(const ProjectArgs a, int n_tt, int n_ct) {
-  using C = Tile<FP8, C0 + C1>;
-  __shared__ __attribute__((aligned(1024))) char ring[C::RING * C::SB];
-  // Workgroup L runs on XCD L % 8; each XCD takes a contiguous eighth of the
-  // tiles, in bands of four token tiles, whose rows of X and columns of W its
-  // L2 then serves several times.
+// Tiles of 256 tokens x 32 (C0 + C1) columns: eight waves, four by tokens (64
+// each) and two by columns (32 C0 and 32 C1 of them), on 32x32 MFMAs.  Waves w
+// and w + 4 share a SIMD, so an uneven pair loads all SIMDs alike.  The operands
+// come through rings in LDS with direct loads that all waves issue: X in three
+// blocks of 128 bytes of k a row (half a line costs a CU as much as a whole one:
+// with 64 bytes a row the loads ran at 31 bytes a clock and bounded the kernel,
+// whole lines run at 63), the weights in four half-blocks.  A wave reads the
+// fragments of its next step between the MFMAs of this one.  X rows are
+// XOR-swizzled in 16-byte chunks, weight rows (as in memory) in blocks of 32
+// columns, so that the rows which one read takes together hit different banks.
+constexpr int TL_T = 256;
+
+template <bool FP8, int NP>  // NP = C0 + C1 column blocks
+struct Tile {
+  static constexpr int E = FP8 ? 1 : 2, KS = 64 / E, KK = FP8 ? 1 : 2;  // bytes; k and MFMA steps of a half-block
+  static constexpr int CT = 32 * NP, WRB = CT * E;                      // columns; bytes of a weight row
+  static constexpr int XB = TL_T * 128, WB = CT * 64;                   // bytes of a block of X, of a half-block of W
+  static constexpr int NW = WB / 1024, NI = 2 + (NW + 7) / 8;           // 1 KB loads of W; of a wave and half-block, at most
+  static constexpr int BYTES = 3 * XB + 4 * WB;
+};
+
+// One wave's part of a tile: tokens t0 + 64 wt .., columns c0 + 32 cb0 .. of CB blocks.
+template <bool FP8, int NP, int CB>
+__device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* ring, int64_t t0, int64_t c0, int cb0) {
+  using C = Tile<FP8, NP>;
+  using M = Mma<FP8>;
+  using Frag = typename M::Frag;
+  constexpr int E = C::E;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wt = wv & 3;
+  const int toks = (int)(a.T - t0 < TL_T ? a.T - t0 : (int64_t)TL_T), d_in = (int)a.d_in;
+  const int32_t ldw = (int32_t)(a.d_out * E), ldx = (int32_t)(a.ld_x * E);
+  const i32x4 rx = buffer_rsrc(static_cast<const char*>(a.X) + t0 * ldx, (toks - 1) * ldx + d_in * E);
+  const i32x4 rw = buffer_rsrc(a.W, d_in * ldw);
+  // A wave's loads of a half-block: two of the 32 of the block of X (8 rows
+  // each), the other two come with the other half; of the weights load wv and
+  // load 8 + wv, where there are as many.
+  const bool full = 8 * (C::NI - 3) + wv < C::NW;
+  int32_t offx[4], kx, offw[C::NI - 2], kw[C::NI - 2];
+  kx = ((lane % 8) ^ (lane / 16 + 4 * (wv & 1))) * 16 / E;  // rows 8 i + lane / 8 swizzle by (row / 2) % 8, i = wv (mod 2)
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int r = (8 * j + wv) * 8 + lane / 8;
+    offx[j] = r < toks ? r * ldx + kx * E : INT32_MIN;
+  }
+#pragma unroll
+  for (int j = 0; j < C::NI - 2; ++j) {
+    const int b = (8 * j + wv) * 1024 + lane * 16, k = b / C::WRB, p = b % C::WRB / (32 * E), in = b % (32 * E) / E;
+    const int64_t col = c0 + (p ^ swz_blocks<FP8, NP>(k)) * 32 + in;
+    kw[j] = k;
+    offw[j] = col < a.d_out ? k * ldw + (int32_t)col * E : INT32_MIN;
+  }
+  static_assert(C::NW % 2 == 0 && C::WRB % 32 == 0 && C::BYTES <= 160 * 1024, "loads, LDS");
+  char* ringw = ring + 3 * C::XB;
+  auto issue_x = [&](int blk, int slot, int part) {
+    char* st = ring + slot * C::XB;
+    const int k0 = blk * 2 * C::KS;
+    const bool whole = k0 + 2 * C::KS <= d_in;  // the k offset is scalar
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int32_t off = part ? offx[2 + j] : offx[j];
+      char* to = st + (8 * (2 * part + j) + wv) * 1024;
+      if (whole) lds_dma16(rx, to, off, k0 * E);
+      else lds_dma16(rx, to, k0 + kx < d_in && off != INT32_MIN ? off + k0 * E : INT32_MIN, 0);
+    }
+  };
+  auto issue_w = [&](int hb, int slot) {
+    char* st = ringw + slot * C::WB;
+    const int k0 = hb * C::KS;
+    const bool whole = k0 + C::KS <= d_in;
+    const uint32_t ks = (uint32_t)k0 * (uint32_t)ldw;
+#pragma unroll
+    for (int j = 0; j < C::NI - 2; ++j) {
+      if (j == C::NI - 3 && !full) break;
+      char* to = st + (8 * j + wv) * 1024;
+      if (whole) lds_dma16(rw, to, offw[j], (int32_t)ks);
+      else lds_dma16(rw, to, k0 + kw[j] < d_in && offw[j] != INT32_MIN ? (int32_t)((uint32_t)offw[j] + ks) : INT32_MIN, 0);
+    }
+  };
+  // Waits until only `n` half-blocks of this wave's loads are in flight.
+  auto wait_halves = [&](auto n) {
+    if (full) wait_loads<decltype(n)::value * C::NI>();
+    else wait_loads<decltype(n)::value * (C::NI - 1)>();
+  };
+
+  const int l32 = lane & 31, h = lane >> 5, grp = lane >> 4, i16 = lane & 15;
+  f32x16 acc[CB][2];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) acc[cb][tb][j] = 0.f;
+  const int xrow = 64 * wt + l32, xs = (xrow >> 1) & 7;  // rows 32 further swizzle alike
+  auto read_x = [&](int tb, const char* st, int c) -> Frag {  // from chunk c of the row's block on
+    const char* p = st + (xrow + 32 * tb) * 128;
+    if constexpr (FP8) {
+      const u32x4 lo = *reinterpret_cast<const u32x4*>(p + ((c + 2 * h) ^ xs) * 16);
+      const u32x4 hi = *reinterpret_cast<const u32x4*>(p + ((c + 2 * h + 1) ^ xs) * 16);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      return *reinterpret_cast<const u32x4*>(p + ((c + h) ^ xs) * 16);
+    }
+  };
+  // First weight row of this lane; the rows it reads besides swizzle alike.
+  const int wk = FP8 ? 32 * h + i16 / 2 : 8 * h + i16 / 4, ws = swz_blocks<FP8, NP>(wk);
+  const int wo = wk * C::WRB + (grp & 1) * 16 * E + (FP8 ? i16 % 2 : i16 % 4) * 8;
+  auto read_w = [&](int cb, const char* st, int kk) -> Frag {
+    const char* p = st + wo + ((cb0 + cb) ^ ws) * (32 * E) + 16 * kk * C::WRB;
+    if constexpr (FP8) {
+      const u32x2 v0 = lds_read_tr8(p), v1 = lds_read_tr8(p + 8 * C::WRB), v2 = lds_read_tr8(p + 16 * C::WRB),
+                  v3 = lds_read_tr8(p + 24 * C::WRB);
+      return Frag{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+    } else {
+      const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * C::WRB);
+      return Frag{lo[0], lo[1], hi[0], hi[1]};
+    }
+  };
+
+  // Half-block s's turn issues half of block s / 2 + 2 of X and half-block s + 3
+  // of W.  The first four turns are ahead of the loop.
+  const int nh = (d_in + C::KS - 1) / C::KS;
+  issue_x(0, 0, 0);
+  issue_x(0, 0, 1);
+  issue_w(0, 0);
+  issue_x(1, 1, 0);
+  issue_w(1, 1);
+  issue_x(1, 1, 1);
+  issue_w(2, 2);
+  wait_halves(std::integral_constant<int, 2>{});
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  Frag fw[CB], fx[2][2];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) fw[cb] = read_w(cb, ringw, 0);
+#pragma unroll
+  for (int tb = 0; tb < 2; ++tb) fx[0][tb] = read_x(tb, ring, 0);
+  int xsl = 0, wsl = 0;  // slots of the block of X and half-block of W in use
+  // Half-block s = 2 b + HALF, its first X fragments in set P0.  A weight
+  // fragment is read again (of the next step) as soon as its last MFMA is issued.
+  auto half = [&](int s, auto HALF, auto P0) {
+    constexpr int hf = decltype(HALF)::value, p0 = decltype(P0)::value;
+    const int wn = wsl + 1 == 4 ? 0 : wsl + 1, xn = xsl + 1 == 3 ? 0 : xsl + 1, xl = xsl == 0 ? 2 : xsl - 1, wl = wsl == 0 ? 3 : wsl - 1;
+    const char* sx = ring + xsl * C::XB;
+    const char* sxn = hf ? ring + xn * C::XB : sx;
+    const char* sw = ringw + wsl * C::WB;
+    const char* swn = ringw + wn * C::WB;
+#pragma unroll
+    for (int kk = 0; kk < C::KK; ++kk) {
+      const int cur = (p0 + kk) & 1, nxt = cur ^ 1;
+      const bool end = kk == C::KK - 1;
+      if (end) {
+        // What half-block s + 1 needs was issued two turns ago or earlier and
+        // has landed; every wave has used what it read of half-block s - 1, so
+        // its slot of W, and the slot of X before this one, are filled again.
+        wait_halves(std::integral_constant<int, 1>{});
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        issue_x(s / 2 + 2, xl, hf);  // past the end: zeros
+        issue_w(s + 3, wl);
+      }
+      const char* rx_ = end ? sxn : sx;
+      const char* rw_ = end ? swn : sw;
+      const int kn = end ? 0 : kk + 1;
+      const int cn = end ? (hf ? 0 : 4) : 4 * hf + 2 * (kk + 1);  // chunk of the next step
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        if (cb < 2) fx[nxt][cb] = read_x(cb, rx_, cn);
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) acc[cb][tb] = M::mma(fw[cb], fx[cur][tb], acc[cb][tb]);
+        fw[cb] = read_w(cb, rw_, kn);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    wsl = wn;
+    if (hf) xsl = xn;
+  };
+  static_assert(CB >= 2, "both X fragments are read");
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, 1>;
+  using IP = std::integral_constant<int, C::KK & 1>;  // the set after one half-block
+  int s = 0;
+  for (; s + 1 < nh; s += 2) {
+    half(s, I0{}, I0{});
+    half(s + 1, I1{}, IP{});
+  }
+  if (s < nh) half(s, I0{}, I0{});
+  wait_loads<0>();
+  wait_lds();
+  __builtin_amdgcn_s_barrier();  // the rings are free
+  asm volatile("" ::: "memory");
+  static_assert(8 * finish_bytes<(NP + 1) / 2, 2> <= C::BYTES, "the waves' results fit the rings");
+  finish_tile<FP8, CB, 2>(a, ksa, acc, ring + wv * finish_bytes<(NP + 1) / 2, 2>, t0 + 64 * wt, c0 + 32 * cb0);
+}
+
+// Workgroup L runs on XCD L % 8; each XCD takes a contiguous eighth of the
+// tiles, in bands of four token tiles, whose rows of X and columns of W its L2
+// then serves several times.  False: past the last tile.
+__device__ __forceinline__ bool my_tile(int n_tt, int n_ct, int& tt, int& ct) {
   const int n_tiles = n_tt * n_ct, per = (n_tiles + 7) / 8;
   const int tile = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
-  if ((int)(blockIdx.x / 8) >= per || tile >= n_tiles) return;  // uniform over the workgroup
+  if ((int)(blockIdx.x / 8) >= per || tile >= n_tiles) return false;
   const int band = tile / (4 * n_ct), in = tile - band * 4 * n_ct, bh = n_tt - 4 * band < 4 ? n_tt - 4 * band : 4;
-  const int ct = __builtin_amdgcn_readfirstlane(in / bh), tt = __builtin_amdgcn_readfirstlane(4 * band + in % bh);
-  const int64_t t0 = (int64_t)tt * TL_T, c0 = (int64_t)ct * C::CT;
-  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) < 4) tile_wave<FP8, C0 + C1, C0>(a, ring, t0, c0, 0);
-  else tile_wave<FP8, C0 + C1, C1>(a, ring, t0, c0, C0);
+  ct = __builtin_amdgcn_readfirstlane(in / bh);
+  tt = __builtin_amdgcn_readfirstlane(4 * band + in % bh);
+  return true;
 }
 
 template <bool FP8, int C0, int C1>
-hipError_t launch_tiles(const ProjectArgs& a, hipStream_t st) {
+__global__ void __launch_bounds__(512, 2) tile_kernel(const ProjectArgs a, int ksa, int n_tt, int n_ct) {
+  using C = Tile<FP8, C0 + C1>;
+  __shared__ __attribute__((aligned(1024))) char ring[C::BYTES];
+  int tt, ct;
+  if (!my_tile(n_tt, n_ct, tt, ct)) return;  // uniform over the workgroup
+  const int64_t t0 = (int64_t)tt * TL_T, c0 = (int64_t)ct * C::CT;
+  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) < 4) tile_wave<FP8, C0 + C1, C0>(a, ksa, ring, t0, c0, 0);
+  else tile_wave<FP8, C0 + C1, C1>(a, ksa, ring, t0, c0, C0);
+}
+
+template <bool FP8, int C0, int C1>
+hipError_t launch_tiles(const ProjectArgs& a, int ksa, hipStream_t st) {
   const int64_t n_tt = (a.T + TL_T - 1) / TL_T, n_ct = (a.d_out + 32 * (C0 + C1) - 1) / (32 * (C0 + C1));
-  hipLaunchKernelGGL((tile_kernel<FP8, C0, C1>), dim3((unsigned)((n_tt * n_ct + 7) / 8 * 8)), dim3(512), 0, st, a, (int)n_tt,
+  hipLaunchKernelGGL((tile_kernel<FP8, C0, C1>), dim3((unsigned)((n_tt * n_ct + 7) / 8 * 8)), dim3(512), 0, st, a, ksa, (int)n_tt,
                      (int)n_ct);
   return hipGetLastError();
 }
@@ -670,8 +830,15 @@ hipError_t launch_tiles(const ProjectArgs& a, hipStream_t st) {
 template <bool FP8>
 hipError_t launch(const ProjectArgs& a, hipStream_t st) {
   if (a.T <= ST_T) return launch_stream<FP8>(a, st);
+  const int ksa = shrink_slices(a.T, a.d_in, a.cus);
   if (a.n_agents > 0) {
-    hipLaunchKernelGGL((shrink_kernel<FP8>), dim3((unsigned)((a.T + 15) / 16)), dim3(ST_W * 64), 0, st, a);
+    const dim3 grid((unsigned)((a.T + 15) / 16 * ksa));
+    switch (a.rank) {
+      case 8: hipLaunchKernelGGL((shrink_kernel<FP8, 8>), grid, dim3(ST_W * 64), 0, st, a, ksa); break;
+      case 16: hipLaunchKernelGGL((shrink_kernel<FP8, 16>), grid, dim3(ST_W * 64), 0, st, a, ksa); break;
+      case 32: hipLaunchKernelGGL((shrink_kernel<FP8, 32>), grid, dim3(ST_W * 64), 0, st, a, ksa); break;
+      default: hipLaunchKernelGGL((shrink_kernel<FP8, 64>), grid, dim3(ST_W * 64), 0, st, a, ksa); break;
+    }
     if (const hipError_t e = hipGetLastError()) return e;
   }
   // The width that takes the least time by rounds of the CUs.
@@ -687,10 +854,10 @@ hipError_t launch(const ProjectArgs& a, hipStream_t st) {
   }
   if (const char* f = getenv("TL_NP")) best = atoi(f);
   switch (best) {
-    case 8: return launch_tiles<FP8, 4, 4>(a, st);
-    case 6: return launch_tiles<FP8, 3, 3>(a, st);
-    case 5: return launch_tiles<FP8, 3, 2>(a, st);
-    default: return launch_tiles<FP8, 2, 2>(a, st);
+    case 8: return launch_tiles<FP8, 4, 4>(a, ksa, st);
+    case 6: return launch_tiles<FP8, 3, 3>(a, ksa, st);
+    case 5: return launch_tiles<FP8, 3, 2>(a, ksa, st);
+    default: return launch_tiles<FP8, 2, 2>(a, ksa, st);
   }
 }
 
@@ -703,7 +870,7 @@ size_t adapted_projection_bytes(int64_t T, int64_t d_in, int64_t d_out, int n_ag
     const size_t b = stream_bytes(T, d_out, rank, stream_plan(T, d_in, d_out, n_agents, rank, true, cus));
     return a > b ? a : b;
   }
-  return n_agents > 0 ? (size_t)T * (size_t)rank * 2 : 0;
+  return n_agents > 0 ? (size_t)shrink_slices(T, d_in, cus) * (size_t)T * (size_t)rank * 4 : 0;
 }
 
 hipError_t launch_adapted_projection(const ProjectArgs& a, hipStream_t st) {
