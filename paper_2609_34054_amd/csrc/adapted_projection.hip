@@ -654,30 +654,21 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
   }
   static_assert(C::NW % 2 == 0 && C::WRB % 32 == 0 && C::BYTES <= 160 * 1024, "loads, LDS");
   char* ringw = ring + 3 * C::XB;
-  auto issue_x = [&](int blk, int slot, int part) {
-    char* st = ring + slot * C::XB;
+  // Load j (0, 1) of part `part` of a block of X; load j of a half-block of W.
+  auto issue_x = [&](int blk, int slot, int part, int j) {
     const int k0 = blk * 2 * C::KS;
-    const bool whole = k0 + 2 * C::KS <= d_in;  // the k offset is scalar
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int32_t off = part ? offx[2 + j] : offx[j];
-      char* to = st + (8 * (2 * part + j) + wv) * 1024;
-      if (whole) lds_dma16(rx, to, off, k0 * E);
-      else lds_dma16(rx, to, k0 + kx < d_in && off != INT32_MIN ? off + k0 * E : INT32_MIN, 0);
-    }
+    const int32_t off = part ? offx[2 + j] : offx[j];
+    char* to = ring + slot * C::XB + (8 * (2 * part + j) + wv) * 1024;
+    if (k0 + 2 * C::KS <= d_in) lds_dma16(rx, to, off, k0 * E);  // whole: the k offset is scalar
+    else lds_dma16(rx, to, k0 + kx < d_in && off != INT32_MIN ? off + k0 * E : INT32_MIN, 0);
   };
-  auto issue_w = [&](int hb, int slot) {
-    char* st = ringw + slot * C::WB;
+  auto issue_w = [&](int hb, int slot, int j) {
+    if (j >= C::NI - 2 || (j == C::NI - 3 && !full)) return;
     const int k0 = hb * C::KS;
-    const bool whole = k0 + C::KS <= d_in;
     const uint32_t ks = (uint32_t)k0 * (uint32_t)ldw;
-#pragma unroll
-    for (int j = 0; j < C::NI - 2; ++j) {
-      if (j == C::NI - 3 && !full) break;
-      char* to = st + (8 * j + wv) * 1024;
-      if (whole) lds_dma16(rw, to, offw[j], (int32_t)ks);
-      else lds_dma16(rw, to, k0 + kw[j] < d_in && offw[j] != INT32_MIN ? (int32_t)((uint32_t)offw[j] + ks) : INT32_MIN, 0);
-    }
+    char* to = ringw + slot * C::WB + (8 * j + wv) * 1024;
+    if (k0 + C::KS <= d_in) lds_dma16(rw, to, offw[j], (int32_t)ks);
+    else lds_dma16(rw, to, k0 + kw[j] < d_in && offw[j] != INT32_MIN ? (int32_t)((uint32_t)offw[j] + ks) : INT32_MIN, 0);
   };
   // Waits until only `n` half-blocks of this wave's loads are in flight.
   auto wait_halves = [&](auto n) {
@@ -720,16 +711,23 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
   };
 
   // Half-block s's turn issues half of block s / 2 + 2 of X and half-block s + 3
-  // of W.  The first four turns are ahead of the loop.
+  // of W, one load at a time between its MFMAs (a CU takes 16 cycles for each,
+  // and a wave that waits for its turn issues nothing else).  With two steps a
+  // half-block the loads of W come in the first step of the next one.
   const int nh = (d_in + C::KS - 1) / C::KS;
-  issue_x(0, 0, 0);
-  issue_x(0, 0, 1);
-  issue_w(0, 0);
-  issue_x(1, 1, 0);
-  issue_w(1, 1);
-  issue_x(1, 1, 1);
-  issue_w(2, 2);
-  wait_halves(std::integral_constant<int, 2>{});
+  auto issue_both = [&](auto f) {
+    f(0);
+    f(1);
+  };
+  issue_both([&](int j) { issue_x(0, 0, 0, j); });
+  issue_both([&](int j) { issue_x(0, 0, 1, j); });
+  issue_both([&](int j) { issue_w(0, 0, j); });
+  issue_both([&](int j) { issue_x(1, 1, 0, j); });
+  issue_both([&](int j) { issue_w(1, 1, j); });
+  issue_both([&](int j) { issue_x(1, 1, 1, j); });
+  if (C::KK == 1) issue_both([&](int j) { issue_w(2, 2, j); });
+  if (full) wait_loads<C::KK == 1 ? 2 * C::NI : C::NI + 2>();
+  else wait_loads<C::KK == 1 ? 2 * C::NI - 2 : C::NI + 1>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   Frag fw[CB], fx[2][2];
@@ -758,8 +756,6 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
         wait_halves(std::integral_constant<int, 1>{});
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        issue_x(s / 2 + 2, xl, hf);  // past the end: zeros
-        issue_w(s + 3, wl);
       }
       const char* rx_ = end ? sxn : sx;
       const char* rw_ = end ? swn : sw;
@@ -771,6 +767,19 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) acc[cb][tb] = M::mma(fw[cb], fx[cur][tb], acc[cb][tb]);
         fw[cb] = read_w(cb, rw_, kn);
+        // Past the end the loads bring zeros.
+        if constexpr (C::KK == 1) {
+          if (cb == 0) issue_x(s / 2 + 2, xl, hf, 0);
+          if (cb == CB / 2) issue_x(s / 2 + 2, xl, hf, 1);
+          if (cb == 1) issue_w(s + 3, wl, 0);
+          if (cb == CB - 1) issue_w(s + 3, wl, 1);
+        } else if (end) {
+          if (cb == 0) issue_x(s / 2 + 2, xl, hf, 0);
+          if (cb == CB / 2) issue_x(s / 2 + 2, xl, hf, 1);
+        } else {
+          if (cb == 0) issue_w(s + 2, wsl < 2 ? wsl + 2 : wsl - 2, 0);
+          if (cb == CB / 2) issue_w(s + 2, wsl < 2 ? wsl + 2 : wsl - 2, 1);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
