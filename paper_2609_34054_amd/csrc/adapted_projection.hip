@@ -327,117 +327,119 @@ hipError_t launch_stream(const ProjectArgs& a, hipStream_t st) {
 // Many rows: X A_a of every row first, then X W in tiles with the expanded
 // adapter rows added as each tile is written.
 //
-// The adapter rows: a workgroup takes 16 rows and a slice of k, its eight waves
-// an eighth of that each, and their agents in turn.  Steps of 128 bytes of k (a
-// CU takes one request of up to 128 bytes every other cycle, so shorter pieces
-// cost as much) come through wave-private rings as above.
-template <bool FP8, int R>
+// The adapter rows: a workgroup takes 64 rows and a slice of k, and as many of
+// their agents at a time as 64 columns hold.  Its stages (128 bytes of k) come
+// through a ring in LDS; every wave computes 16 rows x two blocks of 16 columns.
+// A's rows are short (2 r bytes, and a CU takes one request of up to 128 bytes
+// every other cycle), so A bounds it: 64 rows a workgroup share each of them.
+constexpr int SH_T = 64, SH_NB = 4;  // rows; 16-column blocks
+
+template <bool FP8>
 struct Shrink {
-  static constexpr int KS = FP8 && R < 64 ? 128 : 64;               // k of a step (LDS holds no more at rank 64)
-  static constexpr int XR = KS * (FP8 ? 1 : 2), NC = XR / 16;       // bytes and chunks of a row of X
-  static constexpr int NX = XR / 64, NA = (KS * R * 2 + 1023) / 1024;  // 1 KB loads of X and of A
-  static constexpr int NI = NX + NA, STEP = NI * 1024;
-  static constexpr int RING = 20 / NI < 2 ? 2 : 20 / NI;
-  static_assert(ST_W * RING * STEP <= 160 * 1024, "LDS");
+  static constexpr int E = FP8 ? 1 : 2, KS = 128 / E;          // bytes of an element; k of a stage
+  static constexpr int XB = SH_T * 128, AB = KS * 32;          // bytes of X and of a block of A
+  static constexpr int NA = SH_NB * AB / 8192, NI = 1 + NA;    // a wave's loads of A, and all
+  static constexpr int STEP = XB + SH_NB * AB, RING = FP8 ? 6 : 8;
+  static_assert(RING * STEP <= 160 * 1024, "LDS");
 };
 
-template <bool FP8, int R>
-__global__ void __launch_bounds__(ST_W * 64) shrink_kernel(const ProjectArgs a, int ksa) {
-  using C = Shrink<FP8, R>;
-  constexpr int E = FP8 ? 1 : 2, NB = (R + 15) / 16;
-  __shared__ __attribute__((aligned(1024))) char lds[ST_W * C::RING * C::STEP];
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, c16 = lane & 15;
-  const int ki = (int)(blockIdx.x % (unsigned)ksa);
-  const int64_t t0 = (int64_t)(blockIdx.x / (unsigned)ksa) * 16;
-  const int toks = (int)(a.T - t0 < 16 ? a.T - t0 : (int64_t)16), d_in = (int)a.d_in;
-  const int nk = (d_in + C::KS - 1) / C::KS, part = ki * ST_W + w, parts = ksa * ST_W;
-  const int s_lo = (int)((int64_t)nk * part / parts), s_hi = (int)((int64_t)nk * (part + 1) / parts);
+template <bool FP8>
+__global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ksa) {
+  using C = Shrink<FP8>;
+  constexpr int E = C::E;
+  __shared__ __attribute__((aligned(1024))) char ring[C::RING * C::STEP];
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, c16 = lane & 15;
+  const int ki = (int)(blockIdx.x % (unsigned)ksa), R = a.rank, rp = R < 16 ? 16 : R;
+  const int64_t t0 = (int64_t)(blockIdx.x / (unsigned)ksa) * SH_T;
+  const int toks = (int)(a.T - t0 < SH_T ? a.T - t0 : (int64_t)SH_T), d_in = (int)a.d_in;
+  const int nk = (d_in + C::KS - 1) / C::KS;
+  const int s_lo = (int)((int64_t)nk * ki / ksa), s_hi = (int)((int64_t)nk * (ki + 1) / ksa);
   const int ag = lane < toks ? a.agent[t0 + lane] : -1;
   uint64_t todo = __ballot(ag >= 0 && ag < a.n_agents);  // the same in every wave
   float* H = static_cast<float*>(a.ws) + ((int64_t)ki * a.T + t0) * R;
-  char* ring = lds + w * C::RING * C::STEP;
   const int32_t lda = (int32_t)((int64_t)a.n_agents * R * 2), ldx = (int32_t)(a.ld_x * E);
   const i32x4 ra = buffer_rsrc(a.A, d_in * lda);
   const i32x4 rx = buffer_rsrc(static_cast<const char*>(a.X) + t0 * ldx, (toks - 1) * ldx + d_in * E);
-  // X: 16-byte chunks XOR-swizzled by row.
-  int32_t kx[C::NX], ox[C::NX], ka[C::NA];
-#pragma unroll
-  for (int j = 0; j < C::NX; ++j) {
-    const int t = (j * 64 + lane) / C::NC;
-    kx[j] = ((lane % C::NC) ^ (t % C::NC)) * 16 / E;
-    ox[j] = t < toks ? t * ldx + kx[j] * E : INT32_MIN;
-  }
-#pragma unroll
-  for (int j = 0; j < C::NA; ++j) {
-    const int b = j * 1024 + lane * 16;
-    ka[j] = b < C::KS * R * 2 ? b / (R * 2) : INT32_MAX / 2;  // past the step: zeros
-  }
-  const int32_t ca = lane * 16 % (R * 2);  // a lane's bytes within a row of A are the same in every load
+  // X: rows 8 wv .. of this wave, 16-byte chunks XOR-swizzled by row.
+  const int xr = 8 * wv + lane / 8, kx = ((lane % 8) ^ ((xr >> 1) & 7)) * 16 / E;
+  const int32_t ox = xr < toks ? xr * ldx + kx * E : INT32_MIN;
   while (todo != 0) {
-    const int cur = __builtin_amdgcn_readlane(ag, __builtin_ctzll(todo));
-    const uint64_t mine = __ballot(ag == cur);
-    todo &= ~mine;
-    auto issue = [&](int s) {
-      char* st = ring + (s % C::RING) * C::STEP;
-      const int k0 = s * C::KS, left = s < s_hi ? d_in - k0 : 0;
+    // The agents of blocks 0 .. 3 (-1: none).
+    int id[SH_NB];
 #pragma unroll
-      for (int j = 0; j < C::NX; ++j)
-        lds_dma16(rx, st + j * 1024, kx[j] < left && ox[j] != INT32_MIN ? ox[j] + k0 * E : INT32_MIN, 0);
+    for (int b = 0; b < SH_NB; ++b) {
+      if (b * 16 % rp != 0) {  // another block of the same agent
+        id[b] = b > 0 ? id[b - 1] : -1;
+        continue;
+      }
+      id[b] = todo != 0 ? __builtin_amdgcn_readlane(ag, __builtin_ctzll(todo)) : -1;
+      if (todo != 0) todo &= ~__ballot(ag == id[b]);
+    }
+    // A: rows of 32 bytes, block by block; rows 8 .. 15 of every 16 are stored
+    // with their halves swapped, so that the rows of one read hit different banks.
+    int32_t ka[C::NA], oa[C::NA];
+#pragma unroll
+    for (int j = 0; j < C::NA; ++j) {
+      const int b = (8 * j + wv) * 1024 + lane * 16, blk = b / C::AB, p = b % C::AB / 32, c = blk * 16 % rp + b % 32 / 2;
+      int own = id[0];
+#pragma unroll
+      for (int i = 1; i < SH_NB; ++i) own = blk == i ? id[i] : own;
+      ka[j] = p ^ (((p >> 3) & 1) << 2);
+      oa[j] = own >= 0 && c < R ? ka[j] * lda + (own * R + c) * 2 : INT32_MIN;
+    }
+    auto issue = [&](int s) {
+      char* st = ring + (s - s_lo) % C::RING * C::STEP;
+      const int k0 = s * C::KS, left = s < s_hi ? d_in - k0 : 0;
+      lds_dma16(rx, st + wv * 1024, kx < left && ox != INT32_MIN ? ox + k0 * E : INT32_MIN, 0);
 #pragma unroll
       for (int j = 0; j < C::NA; ++j)
-        lds_dma16(ra, st + (C::NX + j) * 1024,
-                  ka[j] < left ? (int32_t)((uint32_t)(k0 + ka[j]) * (uint32_t)lda + (uint32_t)(cur * R * 2 + ca)) : INT32_MIN, 0);
+        lds_dma16(ra, st + C::XB + (8 * j + wv) * 1024,
+                  ka[j] < left && oa[j] != INT32_MIN ? (int32_t)((uint32_t)oa[j] + (uint32_t)k0 * (uint32_t)lda) : INT32_MIN, 0);
     };
-    f32x4 acc[NB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) acc[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
-    __syncthreads();  // the sums before are read
-    for (int i = 0; i < C::RING; ++i) issue(s_lo + i);
+    // This wave's rows 16 tb .. and blocks cb and cb + 2.
+    const int tb = wv & 3, cb = wv >> 2, row = 16 * tb + c16, xs = (row >> 1) & 7;
+    f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    __syncthreads();  // the stages of the agents before are read
+    for (int i = 0; i < C::RING - 1; ++i) issue(s_lo + i);
     for (int s = s_lo; s < s_hi; ++s) {
-      wait_loads<(C::RING - 1) * C::NI>();
-      const char* st = ring + (s % C::RING) * C::STEP;
+      wait_loads<(C::RING - 2) * C::NI>();
+      wait_lds();
+      __builtin_amdgcn_s_barrier();  // stage s has landed, stage s - 1 is read
+      asm volatile("" ::: "memory");
+      issue(s + C::RING - 1);
+      const char* st = ring + (s - s_lo) % C::RING * C::STEP;
 #pragma unroll
       for (int kk = 0; kk < C::KS / 32; ++kk) {
         bf16x8 x;
-        const char* xp = st + c16 * C::XR;
-        if constexpr (FP8)
-          x = as_bf16x8(bf16_of_e4m3(*reinterpret_cast<const u32x2*>(xp + ((2 * kk + q / 2) ^ (c16 % C::NC)) * 16 + q % 2 * 8)));
-        else
-          x = as_bf16x8(*reinterpret_cast<const u32x4*>(xp + ((4 * kk + q) ^ (c16 % C::NC)) * 16));
+        const char* xp = st + row * 128;
+        if constexpr (FP8) x = as_bf16x8(bf16_of_e4m3(*reinterpret_cast<const u32x2*>(xp + ((2 * kk + q / 2) ^ xs) * 16 + q % 2 * 8)));
+        else x = as_bf16x8(*reinterpret_cast<const u32x4*>(xp + ((4 * kk + q) ^ xs) * 16));
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          // Rank 8: the block's upper columns are the lower ones again, and dropped.
-          const char* p = st + C::NX * 1024 + (32 * kk + 8 * q + c16 / 4) * (R * 2) + nb * 32 + c16 % (R == 8 ? 2 : 4) * 8;
-          const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 8 * R);
-          acc[nb] = mfma16x16x32(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}), x, acc[nb]);
+        for (int i = 0; i < 2; ++i) {
+          if (id[cb + 2 * i] < 0) continue;  // uniform
+          const int r = 8 * q + c16 / 4;
+          const char* p = st + C::XB + (cb + 2 * i) * C::AB + (32 * kk + (r ^ (((r >> 3) & 1) << 2))) * 32 + c16 % 4 * 8;
+          const char* p4 = st + C::XB + (cb + 2 * i) * C::AB + (32 * kk + ((r + 4) ^ (((r >> 3) & 1) << 2))) * 32 + c16 % 4 * 8;
+          const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p4);
+          acc[i] = mfma16x16x32(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}), x, acc[i]);
         }
       }
-      wait_lds();  // this step's slot is free
-      issue(s + C::RING);
     }
     wait_loads<0>();
-    // The waves' sums, added in a fixed order.
-    f32x4* sums = reinterpret_cast<f32x4*>(lds);  // [wave][NB][64]
-    __syncthreads();
+    const int own = row < toks ? a.agent[t0 + row] : -1;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) sums[(w * NB + nb) * 64 + lane] = acc[nb];
-    __syncthreads();
-    for (int u = threadIdx.x; u < NB * 64; u += ST_W * 64) {
-      f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < ST_W; ++i) v += sums[i * NB * 64 + u];
-      const int j = u / 64 * 16 + u / 16 % 4 * 4, t = u % 16;
-      if (j < R && (mine >> t & 1)) *reinterpret_cast<f32x4*>(H + t * R + j) = v;
+    for (int i = 0; i < 2; ++i) {
+      const int j = (cb + 2 * i) * 16 % rp + 4 * q;
+      if (id[cb + 2 * i] >= 0 && own == id[cb + 2 * i] && j < R) *reinterpret_cast<f32x4*>(H + row * R + j) = acc[i];
     }
   }
 }
 
-// k slices of the adapter rows: enough workgroups for the CUs, at most 8, a step
-// a wave at least.
+// k slices of the adapter rows: enough workgroups for the CUs, at most 8, two
+// stages each at least.
 int shrink_slices(int64_t T, int64_t d_in, int cus) {
-  const int64_t rows = (T + 15) / 16;
+  const int64_t rows = (T + SH_T - 1) / SH_T, most = d_in / 256;
   int64_t k = cus / rows;
-  const int64_t most = d_in / (128 * ST_W);
   k = k > most ? most : k;
   return (int)(k < 1 ? 1 : (k > 8 ? 8 : k));
 }
@@ -470,117 +472,160 @@ __device__ __forceinline__ int swz_blocks(int k) {
 }
 
 // What a wave does with its sums acc[cb][tb][j]: column cw + 32 cb + (j / 4) * 8
-// + 4 h + j % 4, token tw + 32 tb + l32.  Scales (e4m3), the expanded adapter
-// rows, the rounding, and Y, by way of `lds` (this wave's) so that each row is
-// written in one piece of 64 CB bytes.
+// + 4 h + j % 4, token tw + 32 tb + l32.
+//
+// The scales of e4m3.
 template <int CB, int TB>
-constexpr int finish_bytes = 32 * TB * (64 * CB + 16);
-
-template <bool FP8, int CB, int TB>
-__device__ __forceinline__ void finish_tile(const ProjectArgs& a, int ksa, f32x16 (&acc)[CB][TB], char* lds, int64_t tw, int64_t cw) {
+__device__ __forceinline__ void scale_tile(const ProjectArgs& a, f32x16 (&acc)[CB][TB], int64_t tw, int64_t cw) {
   const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
   float xsc[TB];
 #pragma unroll
-  for (int tb = 0; tb < TB; ++tb) xsc[tb] = FP8 && tw + 32 * tb + l32 < a.T ? a.x_scale[tw + 32 * tb + l32] : 1.f;
-  if constexpr (FP8) {
+  for (int tb = 0; tb < TB; ++tb) xsc[tb] = tw + 32 * tb + l32 < a.T ? a.x_scale[tw + 32 * tb + l32] : 1.f;
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb)
+  for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-      for (int jg = 0; jg < 4; ++jg) {
-        const int64_t c = cw + 32 * cb + jg * 8 + 4 * h;
-        f32x4 wsc = {0.f, 0.f, 0.f, 0.f};
-        if (c < a.d_out) wsc = *reinterpret_cast<const f32x4*>(a.w_scale + c);
+    for (int jg = 0; jg < 4; ++jg) {
+      const int64_t c = cw + 32 * cb + jg * 8 + 4 * h;
+      f32x4 wsc = {0.f, 0.f, 0.f, 0.f};
+      if (c < a.d_out) wsc = *reinterpret_cast<const f32x4*>(a.w_scale + c);
 #pragma unroll
-        for (int tb = 0; tb < TB; ++tb)
+      for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[cb][tb][4 * jg + i] *= xsc[tb] * wsc[i];
-      }
-  }
-  if (a.n_agents > 0) {
-    // Agents of the wave's tokens in turn.  Where a block of 32 tokens has one
-    // agent (tokens past T go with any), its product is summed in place, else it
-    // is added to that agent's tokens alone, so that what is infinite or NaN in
-    // an adapter stays in the rows that use it.
-    int ag[TB];
-    uint64_t todo[TB], any = 0;
-#pragma unroll
-    for (int tb = 0; tb < TB; ++tb) {
-      const int64_t t = tw + 32 * tb + l32;
-      ag[tb] = t < a.T ? a.agent[t] : -1;
-      todo[tb] = __ballot(ag[tb] >= 0 && ag[tb] < a.n_agents);
-      any |= todo[tb];
+        for (int i = 0; i < 4; ++i) acc[cb][tb][4 * jg + i] *= xsc[tb] * wsc[i];
     }
-    const int R = a.rank, nr = (R + 15) / 16;
-    const float* H = static_cast<const float*>(a.ws);
-    while (any != 0) {
-      int cur = 0;
+}
+
+// The expanded adapter rows: all waves of the tile (TT tokens from t0, NP column
+// blocks from c0) together, four of its agents at a time.  The tile's rows X A_a
+// are summed over the k slices, rounded to bf16 and put into LDS, and each
+// agent's rows of B_a beside them, laid out as the weights are.  Where a block
+// of 32 tokens has one agent (tokens past T go with any) its product is summed
+// in place; else it is added to that agent's tokens alone, so that what is
+// infinite or NaN in an adapter stays in the rows that use it.
+constexpr int EX_A = 4;  // agents at a time
+
+template <int NP, int TT>
+constexpr int expand_bytes = TT * 128 + EX_A * 64 * NP * 64;
+
+template <bool FP8, int NP, int TT, int CB, int TB>
+__device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x16 (&acc)[CB][TB], char* lds, int64_t t0, int tw,
+                                            int64_t c0, int cb0) {
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, h = lane >> 5, grp = lane >> 4, i16 = lane & 15;
+  const int R = a.rank, rp = R < 16 ? 16 : R, nc = rp / 8;  // ranks with padding; 16-byte chunks of a row
+  // Agents of the tile's tokens (four or two a lane) and of this wave's.
+  constexpr int NT = TT / 64;
+  int all[NT], ag[TB];
+  bool any = false;
 #pragma unroll
-      for (int tb = TB - 1; tb >= 0; --tb)
-        if (todo[tb] != 0) cur = __builtin_amdgcn_readlane(ag[tb], __builtin_ctzll(todo[tb]));
-      u32x4 fh[TB][4];  // ranks 16 kk + 8 h .. of token l32 of each block
-      bool mine[TB], whole[TB], some[TB];
-      any = 0;
+  for (int i = 0; i < NT; ++i) {
+    const int64_t t = t0 + 64 * i + lane;
+    all[i] = t < a.T ? a.agent[t] : -1;
+    any = any || (all[i] >= 0 && all[i] < a.n_agents);
+  }
+  if (__ballot(any) == 0) return;  // the same in every wave
+#pragma unroll
+  for (int tb = 0; tb < TB; ++tb) ag[tb] = t0 + tw + 32 * tb + l32 < a.T ? a.agent[t0 + tw + 32 * tb + l32] : -1;
+  auto chunk = [&](int r, int c) {  // where chunk c of row r lies
+    return r * rp * 2 + (nc == 2 ? c : (nc == 4 ? c ^ ((r >> 2) & 3) : c ^ ((r >> 1) & 7))) * 16;
+  };
+  {
+    // Thread tid: 1 / TPT of row tid / TPT.
+    constexpr int TPT = 512 / TT;
+    const int r = tid / TPT;
+    const int64_t t = t0 + r;
+    const int own = t < a.T ? a.agent[t] : -1;
+    const bool ok = own >= 0 && own < a.n_agents;
+    const float* H = static_cast<const float*>(a.ws) + t * R;
+    const float xsc = FP8 && ok ? a.x_scale[t] : 1.f;
+    for (int c = tid % TPT; c < nc; c += TPT) {
+      f32x4 v0 = {0.f, 0.f, 0.f, 0.f}, v1 = {0.f, 0.f, 0.f, 0.f};
+      if (ok && c * 8 < R)
+        for (int k = 0; k < ksa; ++k) {
+          const f32x4* p = reinterpret_cast<const f32x4*>(H + k * a.T * R + c * 8);
+          v0 += p[0];
+          v1 += p[1];
+        }
+      if constexpr (FP8) {
+        v0 *= xsc;
+        v1 *= xsc;
+      }
+      *reinterpret_cast<u32x4*>(lds + chunk(r, c)) =
+          u32x4{pack_bf16(v0[0], v0[1]), pack_bf16(v0[2], v0[3]), pack_bf16(v1[0], v1[1]), pack_bf16(v1[2], v1[3])};
+    }
+  }
+  constexpr int WRB = NP * 64;  // bytes of a row of B
+  char* bs = lds + TT * rp * 2;
+  const int wk = 8 * h + i16 / 4, ws = swz_blocks<false, NP>(wk);
+  const int wo = wk * WRB + (grp & 1) * 32 + i16 % 4 * 8;
+  int last = -1;
+  while (true) {
+    // The next agents in ascending order: the least above `last`, four times.
+    int id[EX_A];
+#pragma unroll
+    for (int g = 0; g < EX_A; ++g) {
+      int m = INT32_MAX;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) m = all[i] > last && all[i] < a.n_agents && all[i] < m ? all[i] : m;
+#pragma unroll
+      for (int x = 1; x < 64; x *= 2) {
+        const int o = __shfl_xor(m, x, kWave);
+        m = o < m ? o : m;
+      }
+      id[g] = __builtin_amdgcn_readfirstlane(m);
+      if (id[g] != INT32_MAX) last = id[g];
+    }
+    if (id[0] == INT32_MAX) break;
+#pragma unroll
+    for (int g = 0; g < EX_A; ++g) {
+      if (id[g] == INT32_MAX) break;
+      const i32x4 rb = buffer_rsrc(a.B + (int64_t)id[g] * R * a.d_out, (int32_t)(R * a.d_out * 2));
+      for (int i = wv; i < rp * NP / 16; i += 8) {
+        const int b = i * 1024 + lane * 16, k = b / WRB, p = b % WRB / 64, in = b % 64 / 2;
+        const int64_t col = c0 + (p ^ swz_blocks<false, NP>(k)) * 32 + in;
+        lds_dma16(rb, bs + g * rp * WRB + i * 1024, k < R && col < a.d_out ? (int32_t)((k * a.d_out + col) * 2) : INT32_MIN, 0);
+      }
+    }
+    wait_loads<0>();
+    __syncthreads();  // rows and agents are in LDS
+#pragma unroll
+    for (int g = 0; g < EX_A; ++g) {
+      if (id[g] == INT32_MAX) break;
 #pragma unroll
       for (int tb = 0; tb < TB; ++tb) {
-        const int64_t t = tw + 32 * tb + l32;
-        mine[tb] = ag[tb] == cur;
-        const uint64_t m = __ballot(mine[tb]);
-        some[tb] = m != 0;
-        todo[tb] &= ~m;
-        any |= todo[tb];
-        whole[tb] = __ballot(mine[tb] || t >= a.T) == ~0ull;
-        if (!some[tb]) continue;  // uniform
+        const bool mine = ag[tb] == id[g];
+        if (__ballot(mine) == 0) continue;
+        const bool whole = __ballot(mine || t0 + tw + 32 * tb + l32 >= a.T) == ~0ull;
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          if (kk >= nr) break;  // uniform
-          f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-          if (mine[tb] && 16 * kk + 8 * h < R)
-            for (int k = 0; k < ksa; ++k) {
-              const f32x4* p = reinterpret_cast<const f32x4*>(H + (k * a.T + t) * R + 16 * kk + 8 * h);
-              v[0] += p[0];
-              v[1] += p[1];
-            }
-          if constexpr (FP8) {
-            v[0] *= xsc[tb];
-            v[1] *= xsc[tb];
-          }
-          fh[tb][kk] = u32x4{pack_bf16(v[0][0], v[0][1]), pack_bf16(v[0][2], v[0][3]), pack_bf16(v[1][0], v[1][1]),
-                             pack_bf16(v[1][2], v[1][3])};
-        }
-      }
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) {
-        const int64_t c = cw + 32 * cb + l32;
-        u32x4 fb[4];  // B_a^T: the same ranks of column l32
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          if (kk >= nr) break;  // uniform
-          const bool ok = c < a.d_out && 16 * kk + 8 * h < R;
-          const uint16_t* bp = a.B + ((int64_t)cur * R + 16 * kk + 8 * h) * a.d_out + c;
-          uint32_t v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = ok ? bp[i * a.d_out] : 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) fb[kk][i] = v[2 * i] | v[2 * i + 1] << 16;
-        }
-#pragma unroll
-        for (int tb = 0; tb < TB; ++tb) {
-          if (!some[tb]) continue;
+        for (int cb = 0; cb < CB; ++cb) {
           f32x16 sum;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) sum[j] = whole[tb] ? acc[cb][tb][j] : 0.f;
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            if (kk >= nr) break;
-            sum = mfma32x32x16(as_bf16x8(fb[kk]), as_bf16x8(fh[tb][kk]), sum);
+          for (int j = 0; j < 16; ++j) sum[j] = whole ? acc[cb][tb][j] : 0.f;
+          for (int kk = 0; kk < rp / 16; ++kk) {
+            const char* p = bs + g * rp * WRB + wo + ((cb0 + cb) ^ ws) * 64 + 16 * kk * WRB;
+            const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * WRB);
+            u32x4 fh = *reinterpret_cast<const u32x4*>(lds + chunk(tw + 32 * tb + l32, 2 * kk + h));
+            if (!mine) fh = u32x4{0u, 0u, 0u, 0u};
+            sum = mfma32x32x16(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}), as_bf16x8(fh), sum);
           }
 #pragma unroll
-          for (int j = 0; j < 16; ++j) acc[cb][tb][j] = whole[tb] ? sum[j] : (mine[tb] ? acc[cb][tb][j] + sum[j] : acc[cb][tb][j]);
+          for (int j = 0; j < 16; ++j) acc[cb][tb][j] = whole ? sum[j] : (mine ? acc[cb][tb][j] + sum[j] : acc[cb][tb][j]);
         }
       }
     }
+    __syncthreads();  // all is read
   }
-  constexpr int RB = 64 * CB + 16;  // padded rows
+}
+
+// Y, by way of `lds` (this wave's, rows padded by 16 bytes), so that each row is
+// written in one piece of 64 CB bytes.
+template <int CB, int TB>
+constexpr int store_bytes = 32 * TB * (64 * CB + 16);
+
+template <int CB, int TB>
+__device__ __forceinline__ void store_tile(const ProjectArgs& a, f32x16 (&acc)[CB][TB], char* lds, int64_t tw, int64_t cw) {
+  const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+  constexpr int RB = 64 * CB + 16;
 #pragma unroll
   for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
@@ -800,8 +845,10 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
   wait_lds();
   __builtin_amdgcn_s_barrier();  // the rings are free
   asm volatile("" ::: "memory");
-  static_assert(8 * finish_bytes<(NP + 1) / 2, 2> <= C::BYTES, "the waves' results fit the rings");
-  finish_tile<FP8, CB, 2>(a, ksa, acc, ring + wv * finish_bytes<(NP + 1) / 2, 2>, t0 + 64 * wt, c0 + 32 * cb0);
+  static_assert(8 * store_bytes<(NP + 1) / 2, 2> <= C::BYTES && expand_bytes<NP, TL_T> <= C::BYTES, "the rings hold these");
+  if constexpr (FP8) scale_tile<CB, 2>(a, acc, t0 + 64 * wt, c0 + 32 * cb0);
+  if (a.n_agents > 0) expand_tile<FP8, NP, TL_T, CB, 2>(a, ksa, acc, ring, t0, 64 * wt, c0, cb0);
+  store_tile<CB, 2>(a, acc, ring + wv * store_bytes<(NP + 1) / 2, 2>, t0 + 64 * wt, c0 + 32 * cb0);
 }
 
 // Workgroup L runs on XCD L % 8; each XCD takes a contiguous eighth of the
@@ -841,13 +888,7 @@ hipError_t launch(const ProjectArgs& a, hipStream_t st) {
   if (a.T <= ST_T) return launch_stream<FP8>(a, st);
   const int ksa = shrink_slices(a.T, a.d_in, a.cus);
   if (a.n_agents > 0) {
-    const dim3 grid((unsigned)((a.T + 15) / 16 * ksa));
-    switch (a.rank) {
-      case 8: hipLaunchKernelGGL((shrink_kernel<FP8, 8>), grid, dim3(ST_W * 64), 0, st, a, ksa); break;
-      case 16: hipLaunchKernelGGL((shrink_kernel<FP8, 16>), grid, dim3(ST_W * 64), 0, st, a, ksa); break;
-      case 32: hipLaunchKernelGGL((shrink_kernel<FP8, 32>), grid, dim3(ST_W * 64), 0, st, a, ksa); break;
-      default: hipLaunchKernelGGL((shrink_kernel<FP8, 64>), grid, dim3(ST_W * 64), 0, st, a, ksa); break;
-    }
+    hipLaunchKernelGGL((shrink_kernel<FP8>), dim3((unsigned)((a.T + SH_T - 1) / SH_T * ksa)), dim3(512), 0, st, a, ksa);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   // The width that takes the least time by rounds of the CUs.
