@@ -883,6 +883,193 @@ hipError_t launch_tiles(const ProjectArgs& a, int ksa, hipStream_t st) {
   return hipGetLastError();
 }
 
+// Tiles of 128 tokens x 32 NP columns, for calls whose larger tiles would leave
+// CUs idle: eight waves, two by tokens (64 each), two by columns, and two by k
+// (each stage's first and second half; waves w and w + 4 share a SIMD, one's
+// reads beside the other's MFMAs).  Stages of 128 bytes of k a row come through
+// one ring.  At the end the two waves of a k pair exchange halves of their sums.
+constexpr int MD_T = 128;
+
+template <bool FP8, int NP>
+struct Mid {
+  static constexpr int E = FP8 ? 1 : 2, KS = 128 / E, KK = FP8 ? 1 : 2;  // bytes; k of a stage; MFMA steps of a wave's half
+  static constexpr int CT = 32 * NP, WRB = CT * E, CB = NP / 2;          // columns; bytes of a weight row; blocks of a wave
+  static constexpr int XB = MD_T * 128, SB = XB + CT * 128;              // bytes of X and of a stage
+  static constexpr int NI = SB / 8192;                                   // 1 KB loads of a wave
+  static constexpr int RING = 160 * 1024 / SB < 6 ? 160 * 1024 / SB : 6;
+  static constexpr int BYTES = RING * SB;
+};
+
+template <bool FP8, int NP>
+__global__ void __launch_bounds__(512, 2) mid_kernel(const ProjectArgs a, int ksa, int n_tt, int n_ct) {
+  using C = Mid<FP8, NP>;
+  using M = Mma<FP8>;
+  using Frag = typename M::Frag;
+  constexpr int E = C::E, CB = C::CB;
+  __shared__ __attribute__((aligned(1024))) char ring[C::BYTES];
+  int tt, ct;
+  if (!my_tile(n_tt, n_ct, tt, ct)) return;  // uniform over the workgroup
+  const int64_t t0 = (int64_t)tt * MD_T, c0 = (int64_t)ct * C::CT;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wt = wv & 1, wc = (wv >> 1) & 1, g = wv >> 2;
+  const int toks = (int)(a.T - t0 < MD_T ? a.T - t0 : (int64_t)MD_T), d_in = (int)a.d_in;
+  const int32_t ldw = (int32_t)(a.d_out * E), ldx = (int32_t)(a.ld_x * E);
+  const i32x4 rx = buffer_rsrc(static_cast<const char*>(a.X) + t0 * ldx, (toks - 1) * ldx + d_in * E);
+  const i32x4 rw = buffer_rsrc(a.W, d_in * ldw);
+  // Load j of this wave is load 8 j + wv of the stage, X rows first.
+  int32_t off[C::NI], kof[C::NI];
+#pragma unroll
+  for (int j = 0; j < C::NI; ++j) {
+    const int b = (8 * j + wv) * 1024 + lane * 16;
+    if (j < C::XB / 8192) {
+      const int r = b / 128, c = (lane % 8) ^ ((r >> 1) & 7);
+      kof[j] = c * 16 / E;
+      off[j] = r < toks ? r * ldx + c * 16 : INT32_MIN;
+    } else {
+      const int k = (b - C::XB) / C::WRB, p = (b - C::XB) % C::WRB / (32 * E), in = b % (32 * E) / E;
+      const int64_t col = c0 + (p ^ swz_blocks<FP8, NP>(k)) * 32 + in;
+      kof[j] = k;
+      off[j] = col < a.d_out ? k * ldw + (int32_t)col * E : INT32_MIN;
+    }
+  }
+  auto issue = [&](int s, int slot, int j) {
+    char* to = ring + slot * C::SB + (8 * j + wv) * 1024;
+    const int k0 = s * C::KS;
+    const bool x = j < C::XB / 8192;
+    const uint32_t ks = (uint32_t)k0 * (uint32_t)(x ? E : ldw);
+    if (k0 + C::KS <= d_in) lds_dma16(x ? rx : rw, to, off[j], (int32_t)ks);  // whole: the k offset is scalar
+    else lds_dma16(x ? rx : rw, to, k0 + kof[j] < d_in && off[j] != INT32_MIN ? (int32_t)((uint32_t)off[j] + ks) : INT32_MIN, 0);
+  };
+  const int l32 = lane & 31, h = lane >> 5, grp = lane >> 4, i16 = lane & 15;
+  f32x16 acc[CB][2];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) acc[cb][tb][j] = 0.f;
+  const int xrow = 64 * wt + l32, xs = (xrow >> 1) & 7;  // rows 32 further swizzle alike
+  auto read_x = [&](int tb, const char* st, int kk) -> Frag {
+    const char* p = st + (xrow + 32 * tb) * 128;
+    if constexpr (FP8) {
+      const u32x4 lo = *reinterpret_cast<const u32x4*>(p + ((4 * g + 2 * h) ^ xs) * 16);
+      const u32x4 hi = *reinterpret_cast<const u32x4*>(p + ((4 * g + 2 * h + 1) ^ xs) * 16);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      return *reinterpret_cast<const u32x4*>(p + ((4 * g + 2 * kk + h) ^ xs) * 16);
+    }
+  };
+  const int wk = (FP8 ? 32 * h + i16 / 2 : 8 * h + i16 / 4), ws = swz_blocks<FP8, NP>(wk);
+  const int wo = C::XB + (wk + g * C::KS / 2) * C::WRB + (grp & 1) * 16 * E + (FP8 ? i16 % 2 : i16 % 4) * 8;
+  auto read_w = [&](int cb, const char* st, int kk) -> Frag {
+    const char* p = st + wo + ((CB * wc + cb) ^ ws) * (32 * E) + 16 * kk * C::WRB;
+    if constexpr (FP8) {
+      const u32x2 v0 = lds_read_tr8(p), v1 = lds_read_tr8(p + 8 * C::WRB), v2 = lds_read_tr8(p + 16 * C::WRB),
+                  v3 = lds_read_tr8(p + 24 * C::WRB);
+      return Frag{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
+    } else {
+      const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * C::WRB);
+      return Frag{lo[0], lo[1], hi[0], hi[1]};
+    }
+  };
+  const int ns = (d_in + C::KS - 1) / C::KS;
+  for (int s = 0; s < C::RING - 1; ++s)
+#pragma unroll
+    for (int j = 0; j < C::NI; ++j) issue(s, s, j);
+  wait_loads<(C::RING - 2) * C::NI>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  Frag fw[2][CB], fx[2][2];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) fw[0][cb] = read_w(cb, ring, 0);
+#pragma unroll
+  for (int tb = 0; tb < 2; ++tb) fx[0][tb] = read_x(tb, ring, 0);
+  int slot = 0, last = C::RING - 1;  // slots of stage s and of stage s - 1
+  auto stage = [&](int s, auto P0) {
+    constexpr int p0 = decltype(P0)::value;
+    const int next = slot + 1 == C::RING ? 0 : slot + 1;
+    const char* st = ring + slot * C::SB;
+    const char* stn = ring + next * C::SB;
+#pragma unroll
+    for (int kk = 0; kk < C::KK; ++kk) {
+      const int cur = (p0 + kk) & 1, nxt = cur ^ 1;
+      const bool end = kk == C::KK - 1;
+      if (end) {
+        // Stage s + 1 has landed, and every wave has used what it read of stage
+        // s - 1, whose slot is filled again.
+        wait_loads<(C::RING - 3) * C::NI>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+      const char* sn = end ? stn : st;
+      const int kn = end ? 0 : kk + 1;
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb) {
+        fx[nxt][tb] = read_x(tb, sn, kn);
+        if (tb < CB) fw[nxt][tb] = read_w(tb, sn, kn);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) acc[cb][tb] = M::mma(fw[cur][cb], fx[cur][tb], acc[cb][tb]);
+        if (end) {  // past the end: zeros
+#pragma unroll
+          for (int j = tb * ((C::NI + 1) / 2); j < (tb ? C::NI : (C::NI + 1) / 2); ++j) issue(s + C::RING - 1, last, j);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    last = slot;
+    slot = next;
+  };
+  using I0 = std::integral_constant<int, 0>;
+  using IP = std::integral_constant<int, C::KK & 1>;
+  int s = 0;
+  for (; s + 1 < ns; s += 2) {
+    stage(s, I0{});
+    stage(s + 1, IP{});
+  }
+  if (s < ns) stage(s, I0{});
+  wait_loads<0>();
+  wait_lds();
+  __builtin_amdgcn_s_barrier();  // the ring is free
+  asm volatile("" ::: "memory");
+  // Waves w and w + 4 hold the two halves of k: the first takes the sums of
+  // token block 0, the second those of block 1.
+  f32x4* ex = reinterpret_cast<f32x4*>(ring);  // [wave][CB][4][64]
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = g ? acc[cb][0][4 * j + i] : acc[cb][1][4 * j + i];
+      ex[((wv * CB + cb) * 4 + j) * 64 + lane] = v;
+    }
+  __syncthreads();
+  f32x16 out[CB][1];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 v = ex[(((wv ^ 4) * CB + cb) * 4 + j) * 64 + lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[cb][0][4 * j + i] = (g ? acc[cb][1][4 * j + i] : acc[cb][0][4 * j + i]) + v[i];
+    }
+  __syncthreads();  // the ring is free again
+  static_assert(8 * store_bytes<CB, 1> <= C::BYTES && expand_bytes<NP, MD_T> <= C::BYTES && 8 * CB * 4096 <= C::BYTES, "the ring holds these");
+  const int tw = 64 * wt + 32 * g;
+  const int64_t cw = c0 + 32 * CB * wc;
+  if constexpr (FP8) scale_tile<CB, 1>(a, out, t0 + tw, cw);
+  if (a.n_agents > 0) expand_tile<FP8, NP, MD_T, CB, 1>(a, ksa, out, ring, t0, tw, c0, CB * wc);
+  store_tile<CB, 1>(a, out, ring + wv * store_bytes<CB, 1>, t0 + tw, cw);
+}
+
+template <bool FP8, int NP>
+hipError_t launch_mid(const ProjectArgs& a, int ksa, hipStream_t st) {
+  const int64_t n_tt = (a.T + MD_T - 1) / MD_T, n_ct = (a.d_out + 32 * NP - 1) / (32 * NP);
+  hipLaunchKernelGGL((mid_kernel<FP8, NP>), dim3((unsigned)((n_tt * n_ct + 7) / 8 * 8)), dim3(512), 0, st, a, ksa, (int)n_tt,
+                     (int)n_ct);
+  return hipGetLastError();
+}
+
 template <bool FP8>
 hipError_t launch(const ProjectArgs& a, hipStream_t st) {
   if (a.T <= ST_T) return launch_stream<FP8>(a, st);
@@ -907,6 +1094,8 @@ hipError_t launch(const ProjectArgs& a, hipStream_t st) {
     case 8: return launch_tiles<FP8, 4, 4>(a, ksa, st);
     case 6: return launch_tiles<FP8, 3, 3>(a, ksa, st);
     case 5: return launch_tiles<FP8, 3, 2>(a, ksa, st);
+    case 14: return launch_mid<FP8, 4>(a, ksa, st);
+    case 12: return launch_mid<FP8, 2>(a, ksa, st);
     default: return launch_tiles<FP8, 2, 2>(a, ksa, st);
   }
 }
