@@ -28,6 +28,23 @@ __device__ __forceinline__ u32x2 lds_read_tr8(const void* p) {
   return __builtin_bit_cast(u32x2, v);
 }
 
+// LDS pointers that stay 32 bits wide, and accesses through them.
+typedef __attribute__((address_space(3))) char lds_char;
+__device__ __forceinline__ u32x4 lds_read16(const lds_char* p) { return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(p); }
+__device__ __forceinline__ u32x2 lds_tr16(const lds_char* p) {
+  typedef short v4s __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s __attribute__((address_space(3)))*)(p)));
+}
+__device__ __forceinline__ u32x2 lds_tr8(const lds_char* p) {
+  typedef int v2i __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((v2i __attribute__((address_space(3)))*)(p)));
+}
+// lds_dma16 with the (wave-uniform) LDS address as a number.
+__device__ __forceinline__ void lds_dma16_at(i32x4 rsrc, uint32_t to, int32_t voff, int32_t soff) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(voff), "s"(rsrc), "s"(soff)
+               : "memory", "m0");
+}
+
 // Waits until at most N of this wave's loads are in flight, or for its LDS
 // reads; memory accesses stay on their side.
 template <int N>
@@ -663,27 +680,34 @@ struct Tile {
   static constexpr int E = FP8 ? 1 : 2, KS = 64 / E, KK = FP8 ? 1 : 2;  // bytes; k and MFMA steps of a half-block
   static constexpr int CT = 32 * NP, WRB = CT * E;                      // columns; bytes of a weight row
   static constexpr int XB = TL_T * 128, WB = CT * 64;                   // bytes of a block of X, of a half-block of W
-  static constexpr int NW = WB / 1024, NI = 2 + (NW + 7) / 8;           // 1 KB loads of W; of a wave and half-block, at most
-  static constexpr int BYTES = 3 * XB + 4 * WB;
+  // 1 KB loads of W of a half-block: N0 by each of waves 0 .. 3, N1 by each of
+  // the others, so that every wave's count is known to the compiler (what
+  // exceeds NW loads zeros past the rings).
+  static constexpr int NW = WB / 1024, N0 = (NW + 7) / 8, N1 = (NW - 4 * N0 + 3) / 4;
+  static constexpr int RINGS = 3 * XB + 4 * WB, BYTES = RINGS + (4 * (N0 + N1) > NW ? 1024 : 0);
 };
 
-// One wave's part of a tile: tokens t0 + 64 wt .., columns c0 + 32 cb0 .. of CB blocks.
-template <bool FP8, int NP, int CB>
-__device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* ring, int64_t t0, int64_t c0, int cb0) {
+// One wave's part of a tile: tokens t0 + 64 wt .., columns c0 + 32 cb0 .. of CB
+// blocks; GRP: waves 0 .. 3 or the others.
+template <bool FP8, int NP, int CB, int GRP>
+__device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* lds, int64_t t0, int64_t c0, int cb0) {
   using C = Tile<FP8, NP>;
   using M = Mma<FP8>;
   using Frag = typename M::Frag;
-  constexpr int E = C::E;
+  constexpr int E = C::E, NWL = GRP == 0 ? C::N0 : C::N1, NI = 2 + NWL;  // loads of W and of all, of this wave and half-block
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wt = wv & 3;
   const int toks = (int)(a.T - t0 < TL_T ? a.T - t0 : (int64_t)TL_T), d_in = (int)a.d_in;
   const int32_t ldw = (int32_t)(a.d_out * E), ldx = (int32_t)(a.ld_x * E);
   const i32x4 rx = buffer_rsrc(static_cast<const char*>(a.X) + t0 * ldx, (toks - 1) * ldx + d_in * E);
   const i32x4 rw = buffer_rsrc(a.W, d_in * ldw);
+  lds_char* const ring = (lds_char*)lds;
+  lds_char* const ringw = ring + 3 * C::XB;
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)ring);
   // A wave's loads of a half-block: two of the 32 of the block of X (8 rows
-  // each), the other two come with the other half; of the weights load wv and
-  // load 8 + wv, where there are as many.
-  const bool full = 8 * (C::NI - 3) + wv < C::NW;
-  int32_t offx[4], kx, offw[C::NI - 2], kw[C::NI - 2];
+  // each), the other two come with the other half; and its loads of W.
+  int32_t offx[4], kx, offw[NWL], kw[NWL];
+  uint32_t tow[NWL];  // LDS address in slot 0
+  bool in_ring[NWL];
   kx = ((lane % 8) ^ (lane / 16 + 4 * (wv & 1))) * 16 / E;  // rows 8 i + lane / 8 swizzle by (row / 2) % 8, i = wv (mod 2)
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -691,34 +715,31 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
     offx[j] = r < toks ? r * ldx + kx * E : INT32_MIN;
   }
 #pragma unroll
-  for (int j = 0; j < C::NI - 2; ++j) {
-    const int b = (8 * j + wv) * 1024 + lane * 16, k = b / C::WRB, p = b % C::WRB / (32 * E), in = b % (32 * E) / E;
+  for (int j = 0; j < NWL; ++j) {
+    const int i = (GRP == 0 ? 0 : 4 * C::N0) + 4 * j + wt, b = i * 1024 + lane * 16, k = b / C::WRB, p = b % C::WRB / (32 * E),
+              in = b % (32 * E) / E;
     const int64_t col = c0 + (p ^ swz_blocks<FP8, NP>(k)) * 32 + in;
     kw[j] = k;
-    offw[j] = col < a.d_out ? k * ldw + (int32_t)col * E : INT32_MIN;
+    in_ring[j] = i < C::NW;
+    offw[j] = i < C::NW && col < a.d_out ? k * ldw + (int32_t)col * E : INT32_MIN;
+    tow[j] = at + (i < C::NW ? 3 * C::XB + i * 1024 : C::RINGS);
   }
-  static_assert(C::NW % 2 == 0 && C::WRB % 32 == 0 && C::BYTES <= 160 * 1024, "loads, LDS");
-  char* ringw = ring + 3 * C::XB;
-  // Load j (0, 1) of part `part` of a block of X; load j of a half-block of W.
-  auto issue_x = [&](int blk, int slot, int part, int j) {
+  static_assert(C::WRB % 32 == 0 && C::BYTES <= 160 * 1024 && 4 * (C::N0 + C::N1) >= C::NW, "loads, LDS");
+  // Load j (0, 1) of part `part` of block `blk` of X; load j of half-block hb of
+  // W.  WHOLE: all of its k are below d_in, and the k offset is scalar.
+  auto issue_x = [&](auto WHOLE, int blk, int slot, int part, int j) {
     const int k0 = blk * 2 * C::KS;
     const int32_t off = part ? offx[2 + j] : offx[j];
-    char* to = ring + slot * C::XB + (8 * (2 * part + j) + wv) * 1024;
-    if (k0 + 2 * C::KS <= d_in) lds_dma16(rx, to, off, k0 * E);  // whole: the k offset is scalar
-    else lds_dma16(rx, to, k0 + kx < d_in && off != INT32_MIN ? off + k0 * E : INT32_MIN, 0);
+    const uint32_t to = at + slot * C::XB + (8 * (2 * part + j) + wv) * 1024;
+    if constexpr (decltype(WHOLE)::value) lds_dma16_at(rx, to, off, k0 * E);
+    else lds_dma16_at(rx, to, k0 + kx < d_in && off != INT32_MIN ? off + k0 * E : INT32_MIN, 0);
   };
-  auto issue_w = [&](int hb, int slot, int j) {
-    if (j >= C::NI - 2 || (j == C::NI - 3 && !full)) return;
+  auto issue_w = [&](auto WHOLE, int hb, int slot, int j) {
+    if (j >= NWL) return;
     const int k0 = hb * C::KS;
-    const uint32_t ks = (uint32_t)k0 * (uint32_t)ldw;
-    char* to = ringw + slot * C::WB + (8 * j + wv) * 1024;
-    if (k0 + C::KS <= d_in) lds_dma16(rw, to, offw[j], (int32_t)ks);
-    else lds_dma16(rw, to, k0 + kw[j] < d_in && offw[j] != INT32_MIN ? (int32_t)((uint32_t)offw[j] + ks) : INT32_MIN, 0);
-  };
-  // Waits until only `n` half-blocks of this wave's loads are in flight.
-  auto wait_halves = [&](auto n) {
-    if (full) wait_loads<decltype(n)::value * C::NI>();
-    else wait_loads<decltype(n)::value * (C::NI - 1)>();
+    const uint32_t ks = (uint32_t)k0 * (uint32_t)ldw, to = tow[j] + (in_ring[j] ? slot * C::WB : 0);
+    if constexpr (decltype(WHOLE)::value) lds_dma16_at(rw, to, offw[j], (int32_t)ks);
+    else lds_dma16_at(rw, to, k0 + kw[j] < d_in && offw[j] != INT32_MIN ? (int32_t)((uint32_t)offw[j] + ks) : INT32_MIN, 0);
   };
 
   const int l32 = lane & 31, h = lane >> 5, grp = lane >> 4, i16 = lane & 15;
@@ -730,27 +751,28 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
 #pragma unroll
       for (int j = 0; j < 16; ++j) acc[cb][tb][j] = 0.f;
   const int xrow = 64 * wt + l32, xs = (xrow >> 1) & 7;  // rows 32 further swizzle alike
-  auto read_x = [&](int tb, const char* st, int c) -> Frag {  // from chunk c of the row's block on
-    const char* p = st + (xrow + 32 * tb) * 128;
+  const int xo = xrow * 128 + ((FP8 ? 2 * h : h) ^ xs) * 16;  // chunk c + i of the row lies at (xo ^ 16 c) ^ 16 i
+  auto read_x = [&](int tb, const lds_char* st, int c) -> Frag {  // from chunk c of the row's block on
+    const lds_char* p = st + (xo ^ (c * 16)) + 32 * tb * 128;
     if constexpr (FP8) {
-      const u32x4 lo = *reinterpret_cast<const u32x4*>(p + ((c + 2 * h) ^ xs) * 16);
-      const u32x4 hi = *reinterpret_cast<const u32x4*>(p + ((c + 2 * h + 1) ^ xs) * 16);
+      const u32x4 lo = lds_read16(p), hi = lds_read16(st + (xo ^ (c * 16 + 16)) + 32 * tb * 128);
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      return *reinterpret_cast<const u32x4*>(p + ((c + h) ^ xs) * 16);
+      return lds_read16(p);
     }
   };
   // First weight row of this lane; the rows it reads besides swizzle alike.
   const int wk = FP8 ? 32 * h + i16 / 2 : 8 * h + i16 / 4, ws = swz_blocks<FP8, NP>(wk);
-  const int wo = wk * C::WRB + (grp & 1) * 16 * E + (FP8 ? i16 % 2 : i16 % 4) * 8;
-  auto read_w = [&](int cb, const char* st, int kk) -> Frag {
-    const char* p = st + wo + ((cb0 + cb) ^ ws) * (32 * E) + 16 * kk * C::WRB;
+  int wo[CB];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) wo[cb] = wk * C::WRB + (grp & 1) * 16 * E + (FP8 ? i16 % 2 : i16 % 4) * 8 + ((cb0 + cb) ^ ws) * (32 * E);
+  auto read_w = [&](int cb, const lds_char* st, int kk) -> Frag {
+    const lds_char* p = st + wo[cb] + 16 * kk * C::WRB;
     if constexpr (FP8) {
-      const u32x2 v0 = lds_read_tr8(p), v1 = lds_read_tr8(p + 8 * C::WRB), v2 = lds_read_tr8(p + 16 * C::WRB),
-                  v3 = lds_read_tr8(p + 24 * C::WRB);
+      const u32x2 v0 = lds_tr8(p), v1 = lds_tr8(p + 8 * C::WRB), v2 = lds_tr8(p + 16 * C::WRB), v3 = lds_tr8(p + 24 * C::WRB);
       return Frag{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
     } else {
-      const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * C::WRB);
+      const u32x2 lo = lds_tr16(p), hi = lds_tr16(p + 4 * C::WRB);
       return Frag{lo[0], lo[1], hi[0], hi[1]};
     }
   };
@@ -759,20 +781,26 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
   // of W, one load at a time between its MFMAs (a CU takes 16 cycles for each,
   // and a wave that waits for its turn issues nothing else).  With two steps a
   // half-block the loads of W come in the first step of the next one.
+  using T1 = std::true_type;
+  using T0 = std::false_type;
   const int nh = (d_in + C::KS - 1) / C::KS;
-  auto issue_both = [&](auto f) {
-    f(0);
-    f(1);
-  };
-  issue_both([&](int j) { issue_x(0, 0, 0, j); });
-  issue_both([&](int j) { issue_x(0, 0, 1, j); });
-  issue_both([&](int j) { issue_w(0, 0, j); });
-  issue_both([&](int j) { issue_x(1, 1, 0, j); });
-  issue_both([&](int j) { issue_w(1, 1, j); });
-  issue_both([&](int j) { issue_x(1, 1, 1, j); });
-  if (C::KK == 1) issue_both([&](int j) { issue_w(2, 2, j); });
-  if (full) wait_loads<C::KK == 1 ? 2 * C::NI : C::NI + 2>();
-  else wait_loads<C::KK == 1 ? 2 * C::NI - 2 : C::NI + 1>();
+#pragma unroll
+  for (int j = 0; j < 2; ++j) issue_x(T0{}, 0, 0, 0, j);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) issue_x(T0{}, 0, 0, 1, j);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) issue_w(T0{}, 0, 0, j);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) issue_x(T0{}, 1, 1, 0, j);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) issue_w(T0{}, 1, 1, j);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) issue_x(T0{}, 1, 1, 1, j);
+  if constexpr (C::KK == 1) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) issue_w(T0{}, 2, 2, j);
+  }
+  wait_loads<C::KK == 1 ? 2 * NI : NI + 2>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   Frag fw[CB], fx[2][2];
@@ -783,13 +811,13 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
   int xsl = 0, wsl = 0;  // slots of the block of X and half-block of W in use
   // Half-block s = 2 b + HALF, its first X fragments in set P0.  A weight
   // fragment is read again (of the next step) as soon as its last MFMA is issued.
-  auto half = [&](int s, auto HALF, auto P0) {
+  auto half = [&](int s, auto HALF, auto P0, auto WHOLE) {
     constexpr int hf = decltype(HALF)::value, p0 = decltype(P0)::value;
-    const int wn = wsl + 1 == 4 ? 0 : wsl + 1, xn = xsl + 1 == 3 ? 0 : xsl + 1, xl = xsl == 0 ? 2 : xsl - 1, wl = wsl == 0 ? 3 : wsl - 1;
-    const char* sx = ring + xsl * C::XB;
-    const char* sxn = hf ? ring + xn * C::XB : sx;
-    const char* sw = ringw + wsl * C::WB;
-    const char* swn = ringw + wn * C::WB;
+    const int wn = (wsl + 1) & 3, xn = xsl == 2 ? 0 : xsl + 1, xl = xsl == 0 ? 2 : xsl - 1, wl = (wsl + 3) & 3;
+    const lds_char* sx = ring + xsl * C::XB;
+    const lds_char* sxn = hf ? ring + xn * C::XB : sx;
+    const lds_char* sw = ringw + wsl * C::WB;
+    const lds_char* swn = ringw + wn * C::WB;
 #pragma unroll
     for (int kk = 0; kk < C::KK; ++kk) {
       const int cur = (p0 + kk) & 1, nxt = cur ^ 1;
@@ -798,12 +826,12 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
         // What half-block s + 1 needs was issued two turns ago or earlier and
         // has landed; every wave has used what it read of half-block s - 1, so
         // its slot of W, and the slot of X before this one, are filled again.
-        wait_halves(std::integral_constant<int, 1>{});
+        wait_loads<NI>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
       }
-      const char* rx_ = end ? sxn : sx;
-      const char* rw_ = end ? swn : sw;
+      const lds_char* rx_ = end ? sxn : sx;
+      const lds_char* rw_ = end ? swn : sw;
       const int kn = end ? 0 : kk + 1;
       const int cn = end ? (hf ? 0 : 4) : 4 * hf + 2 * (kk + 1);  // chunk of the next step
 #pragma unroll
@@ -814,16 +842,16 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
         fw[cb] = read_w(cb, rw_, kn);
         // Past the end the loads bring zeros.
         if constexpr (C::KK == 1) {
-          if (cb == 0) issue_x(s / 2 + 2, xl, hf, 0);
-          if (cb == CB / 2) issue_x(s / 2 + 2, xl, hf, 1);
-          if (cb == 1) issue_w(s + 3, wl, 0);
-          if (cb == CB - 1) issue_w(s + 3, wl, 1);
+          if (cb == 0) issue_x(WHOLE, s / 2 + 2, xl, hf, 0);
+          if (cb == CB / 2) issue_x(WHOLE, s / 2 + 2, xl, hf, 1);
+          if (cb == 1) issue_w(WHOLE, s + 3, wl, 0);
+          if (cb == CB - 1) issue_w(WHOLE, s + 3, wl, 1);
         } else if (end) {
-          if (cb == 0) issue_x(s / 2 + 2, xl, hf, 0);
-          if (cb == CB / 2) issue_x(s / 2 + 2, xl, hf, 1);
+          if (cb == 0) issue_x(WHOLE, s / 2 + 2, xl, hf, 0);
+          if (cb == CB / 2) issue_x(WHOLE, s / 2 + 2, xl, hf, 1);
         } else {
-          if (cb == 0) issue_w(s + 2, wsl < 2 ? wsl + 2 : wsl - 2, 0);
-          if (cb == CB / 2) issue_w(s + 2, wsl < 2 ? wsl + 2 : wsl - 2, 1);
+          if (cb == 0) issue_w(WHOLE, s + 2, (wsl + 2) & 3, 0);
+          if (cb == CB / 2) issue_w(WHOLE, s + 2, (wsl + 2) & 3, 1);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -836,19 +864,24 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* r
   using I1 = std::integral_constant<int, 1>;
   using IP = std::integral_constant<int, C::KK & 1>;  // the set after one half-block
   int s = 0;
-  for (; s + 1 < nh; s += 2) {
-    half(s, I0{}, I0{});
-    half(s + 1, I1{}, IP{});
+  // Half-blocks s and s + 1 issue X up to k = (s + 6) KS and W up to (s + 5) KS.
+  for (; (s + 6) * C::KS <= d_in; s += 2) {
+    half(s, I0{}, I0{}, T1{});
+    half(s + 1, I1{}, IP{}, T1{});
   }
-  if (s < nh) half(s, I0{}, I0{});
+  for (; s + 1 < nh; s += 2) {
+    half(s, I0{}, I0{}, T0{});
+    half(s + 1, I1{}, IP{}, T0{});
+  }
+  if (s < nh) half(s, I0{}, I0{}, T0{});
   wait_loads<0>();
   wait_lds();
   __builtin_amdgcn_s_barrier();  // the rings are free
   asm volatile("" ::: "memory");
   static_assert(8 * store_bytes<(NP + 1) / 2, 2> <= C::BYTES && expand_bytes<NP, TL_T> <= C::BYTES, "the rings hold these");
   if constexpr (FP8) scale_tile<CB, 2>(a, acc, t0 + 64 * wt, c0 + 32 * cb0);
-  if (a.n_agents > 0) expand_tile<FP8, NP, TL_T, CB, 2>(a, ksa, acc, ring, t0, 64 * wt, c0, cb0);
-  store_tile<CB, 2>(a, acc, ring + wv * store_bytes<(NP + 1) / 2, 2>, t0 + 64 * wt, c0 + 32 * cb0);
+  if (a.n_agents > 0) expand_tile<FP8, NP, TL_T, CB, 2>(a, ksa, acc, lds, t0, 64 * wt, c0, cb0);
+  store_tile<CB, 2>(a, acc, lds + wv * store_bytes<(NP + 1) / 2, 2>, t0 + 64 * wt, c0 + 32 * cb0);
 }
 
 // Workgroup L runs on XCD L % 8; each XCD takes a contiguous eighth of the
@@ -871,8 +904,8 @@ __global__ void __launch_bounds__(512, 2) tile_kernel(const ProjectArgs a, int k
   int tt, ct;
   if (!my_tile(n_tt, n_ct, tt, ct)) return;  // uniform over the workgroup
   const int64_t t0 = (int64_t)tt * TL_T, c0 = (int64_t)ct * C::CT;
-  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) < 4) tile_wave<FP8, C0 + C1, C0>(a, ksa, ring, t0, c0, 0);
-  else tile_wave<FP8, C0 + C1, C1>(a, ksa, ring, t0, c0, C0);
+  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) < 4) tile_wave<FP8, C0 + C1, C0, 0>(a, ksa, ring, t0, c0, 0);
+  else tile_wave<FP8, C0 + C1, C1, 1>(a, ksa, ring, t0, c0, C0);
 }
 
 template <bool FP8, int C0, int C1>
@@ -932,13 +965,16 @@ __global__ void __launch_bounds__(512, 2) mid_kernel(const ProjectArgs a, int ks
       off[j] = col < a.d_out ? k * ldw + (int32_t)col * E : INT32_MIN;
     }
   }
-  auto issue = [&](int s, int slot, int j) {
-    char* to = ring + slot * C::SB + (8 * j + wv) * 1024;
+  lds_char* const lds = (lds_char*)ring;
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)lds);
+  // WHOLE: all k of the stage are below d_in, and the k offset is scalar.
+  auto issue = [&](auto WHOLE, int s, int slot, int j) {
+    const uint32_t to = at + slot * C::SB + (8 * j + wv) * 1024;
     const int k0 = s * C::KS;
     const bool x = j < C::XB / 8192;
     const uint32_t ks = (uint32_t)k0 * (uint32_t)(x ? E : ldw);
-    if (k0 + C::KS <= d_in) lds_dma16(x ? rx : rw, to, off[j], (int32_t)ks);  // whole: the k offset is scalar
-    else lds_dma16(x ? rx : rw, to, k0 + kof[j] < d_in && off[j] != INT32_MIN ? (int32_t)((uint32_t)off[j] + ks) : INT32_MIN, 0);
+    if constexpr (decltype(WHOLE)::value) lds_dma16_at(x ? rx : rw, to, off[j], (int32_t)ks);
+    else lds_dma16_at(x ? rx : rw, to, k0 + kof[j] < d_in && off[j] != INT32_MIN ? (int32_t)((uint32_t)off[j] + ks) : INT32_MIN, 0);
   };
   const int l32 = lane & 31, h = lane >> 5, grp = lane >> 4, i16 = lane & 15;
   f32x16 acc[CB][2];
@@ -949,47 +985,48 @@ __global__ void __launch_bounds__(512, 2) mid_kernel(const ProjectArgs a, int ks
 #pragma unroll
       for (int j = 0; j < 16; ++j) acc[cb][tb][j] = 0.f;
   const int xrow = 64 * wt + l32, xs = (xrow >> 1) & 7;  // rows 32 further swizzle alike
-  auto read_x = [&](int tb, const char* st, int kk) -> Frag {
-    const char* p = st + (xrow + 32 * tb) * 128;
+  const int xo = xrow * 128 + ((4 * g + (FP8 ? 2 * h : h)) ^ xs) * 16;  // chunk c further on lies at xo ^ 16 c
+  auto read_x = [&](int tb, const lds_char* st, int kk) -> Frag {
     if constexpr (FP8) {
-      const u32x4 lo = *reinterpret_cast<const u32x4*>(p + ((4 * g + 2 * h) ^ xs) * 16);
-      const u32x4 hi = *reinterpret_cast<const u32x4*>(p + ((4 * g + 2 * h + 1) ^ xs) * 16);
+      const u32x4 lo = lds_read16(st + xo + 32 * tb * 128), hi = lds_read16(st + (xo ^ 16) + 32 * tb * 128);
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      return *reinterpret_cast<const u32x4*>(p + ((4 * g + 2 * kk + h) ^ xs) * 16);
+      return lds_read16(st + (xo ^ (32 * kk)) + 32 * tb * 128);
     }
   };
   const int wk = (FP8 ? 32 * h + i16 / 2 : 8 * h + i16 / 4), ws = swz_blocks<FP8, NP>(wk);
-  const int wo = C::XB + (wk + g * C::KS / 2) * C::WRB + (grp & 1) * 16 * E + (FP8 ? i16 % 2 : i16 % 4) * 8;
-  auto read_w = [&](int cb, const char* st, int kk) -> Frag {
-    const char* p = st + wo + ((CB * wc + cb) ^ ws) * (32 * E) + 16 * kk * C::WRB;
+  int wo[CB];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+    wo[cb] = C::XB + (wk + g * C::KS / 2) * C::WRB + (grp & 1) * 16 * E + (FP8 ? i16 % 2 : i16 % 4) * 8 + ((CB * wc + cb) ^ ws) * (32 * E);
+  auto read_w = [&](int cb, const lds_char* st, int kk) -> Frag {
+    const lds_char* p = st + wo[cb] + 16 * kk * C::WRB;
     if constexpr (FP8) {
-      const u32x2 v0 = lds_read_tr8(p), v1 = lds_read_tr8(p + 8 * C::WRB), v2 = lds_read_tr8(p + 16 * C::WRB),
-                  v3 = lds_read_tr8(p + 24 * C::WRB);
+      const u32x2 v0 = lds_tr8(p), v1 = lds_tr8(p + 8 * C::WRB), v2 = lds_tr8(p + 16 * C::WRB), v3 = lds_tr8(p + 24 * C::WRB);
       return Frag{v0[0], v0[1], v1[0], v1[1], v2[0], v2[1], v3[0], v3[1]};
     } else {
-      const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * C::WRB);
+      const u32x2 lo = lds_tr16(p), hi = lds_tr16(p + 4 * C::WRB);
       return Frag{lo[0], lo[1], hi[0], hi[1]};
     }
   };
   const int ns = (d_in + C::KS - 1) / C::KS;
   for (int s = 0; s < C::RING - 1; ++s)
 #pragma unroll
-    for (int j = 0; j < C::NI; ++j) issue(s, s, j);
+    for (int j = 0; j < C::NI; ++j) issue(std::false_type{}, s, s, j);
   wait_loads<(C::RING - 2) * C::NI>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   Frag fw[2][CB], fx[2][2];
 #pragma unroll
-  for (int cb = 0; cb < CB; ++cb) fw[0][cb] = read_w(cb, ring, 0);
+  for (int cb = 0; cb < CB; ++cb) fw[0][cb] = read_w(cb, lds, 0);
 #pragma unroll
-  for (int tb = 0; tb < 2; ++tb) fx[0][tb] = read_x(tb, ring, 0);
+  for (int tb = 0; tb < 2; ++tb) fx[0][tb] = read_x(tb, lds, 0);
   int slot = 0, last = C::RING - 1;  // slots of stage s and of stage s - 1
-  auto stage = [&](int s, auto P0) {
+  auto stage = [&](int s, auto P0, auto WHOLE) {
     constexpr int p0 = decltype(P0)::value;
     const int next = slot + 1 == C::RING ? 0 : slot + 1;
-    const char* st = ring + slot * C::SB;
-    const char* stn = ring + next * C::SB;
+    const lds_char* st = lds + slot * C::SB;
+    const lds_char* stn = lds + next * C::SB;
 #pragma unroll
     for (int kk = 0; kk < C::KK; ++kk) {
       const int cur = (p0 + kk) & 1, nxt = cur ^ 1;
@@ -1001,7 +1038,7 @@ __global__ void __launch_bounds__(512, 2) mid_kernel(const ProjectArgs a, int ks
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
       }
-      const char* sn = end ? stn : st;
+      const lds_char* sn = end ? stn : st;
       const int kn = end ? 0 : kk + 1;
 #pragma unroll
       for (int tb = 0; tb < 2; ++tb) {
@@ -1011,7 +1048,7 @@ __global__ void __launch_bounds__(512, 2) mid_kernel(const ProjectArgs a, int ks
         for (int cb = 0; cb < CB; ++cb) acc[cb][tb] = M::mma(fw[cur][cb], fx[cur][tb], acc[cb][tb]);
         if (end) {  // past the end: zeros
 #pragma unroll
-          for (int j = tb * ((C::NI + 1) / 2); j < (tb ? C::NI : (C::NI + 1) / 2); ++j) issue(s + C::RING - 1, last, j);
+          for (int j = tb * ((C::NI + 1) / 2); j < (tb ? C::NI : (C::NI + 1) / 2); ++j) issue(WHOLE, s + C::RING - 1, last, j);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -1022,11 +1059,15 @@ __global__ void __launch_bounds__(512, 2) mid_kernel(const ProjectArgs a, int ks
   using I0 = std::integral_constant<int, 0>;
   using IP = std::integral_constant<int, C::KK & 1>;
   int s = 0;
-  for (; s + 1 < ns; s += 2) {
-    stage(s, I0{});
-    stage(s + 1, IP{});
+  for (; (s + 1 + C::RING) * C::KS <= d_in; s += 2) {
+    stage(s, I0{}, std::true_type{});
+    stage(s + 1, IP{}, std::true_type{});
   }
-  if (s < ns) stage(s, I0{});
+  for (; s + 1 < ns; s += 2) {
+    stage(s, I0{}, std::false_type{});
+    stage(s + 1, IP{}, std::false_type{});
+  }
+  if (s < ns) stage(s, I0{}, std::false_type{});
   wait_loads<0>();
   wait_lds();
   __builtin_amdgcn_s_barrier();  // the ring is free
