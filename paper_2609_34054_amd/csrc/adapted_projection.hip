@@ -836,7 +836,10 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* l
       const int cn = end ? (hf ? 0 : 4) : 4 * hf + 2 * (kk + 1);  // chunk of the next step
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
-        if (cb < 2) fx[nxt][cb] = read_x(cb, rx_, cn);
+        if (cb == 0) {
+          fx[nxt][0] = read_x(0, rx_, cn);
+          fx[nxt][1] = read_x(1, rx_, cn);
+        }
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) acc[cb][tb] = M::mma(fw[cb], fx[cur][tb], acc[cb][tb]);
         fw[cb] = read_w(cb, rw_, kn);
@@ -859,7 +862,6 @@ __device__ __forceinline__ void tile_wave(const ProjectArgs& a, int ksa, char* l
     wsl = wn;
     if (hf) xsl = xn;
   };
-  static_assert(CB >= 2, "both X fragments are read");
   using I0 = std::integral_constant<int, 0>;
   using I1 = std::integral_constant<int, 1>;
   using IP = std::integral_constant<int, C::KK & 1>;  // the set after one half-block
@@ -1042,8 +1044,13 @@ __global__ void __launch_bounds__(512, 2) mid_kernel(const ProjectArgs a, int ks
       const int kn = end ? 0 : kk + 1;
 #pragma unroll
       for (int tb = 0; tb < 2; ++tb) {
-        fx[nxt][tb] = read_x(tb, sn, kn);
-        if (tb < CB) fw[nxt][tb] = read_w(tb, sn, kn);
+        if (tb == 0) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (i < CB) fw[nxt][i] = read_w(i, sn, kn);
+            fx[nxt][i] = read_x(i, sn, kn);
+          }
+        }
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) acc[cb][tb] = M::mma(fw[cur][cb], fx[cur][tb], acc[cb][tb]);
         if (end) {  // past the end: zeros
