@@ -354,9 +354,9 @@ constexpr int SH_T = 64, SH_NB = 4;  // rows; 16-column blocks
 template <bool FP8>
 struct Shrink {
   static constexpr int E = FP8 ? 1 : 2, KS = 128 / E;          // bytes of an element; k of a stage
-  static constexpr int XB = SH_T * 128, AB = KS * 32;          // bytes of X and of a block of A
-  static constexpr int NA = SH_NB * AB / 8192, NI = 1 + NA;    // a wave's loads of A, and all
-  static constexpr int STEP = XB + SH_NB * AB, RING = FP8 ? 6 : 8;
+  static constexpr int XB = SH_T * 128, AB = KS * SH_NB * 32;  // bytes of X and of A
+  static constexpr int NA = AB / 8192, NI = 1 + NA;            // a wave's loads of A, and all
+  static constexpr int STEP = XB + AB, RING = FP8 ? 6 : 8;
   static_assert(RING * STEP <= 160 * 1024, "LDS");
 };
 
@@ -392,38 +392,42 @@ __global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ks
       id[b] = todo != 0 ? __builtin_amdgcn_readlane(ag, __builtin_ctzll(todo)) : -1;
       if (todo != 0) todo &= ~__ballot(ag == id[b]);
     }
-    // A: rows of 32 bytes, block by block; rows 8 .. 15 of every 16 are stored
-    // with their halves swapped, so that the rows of one read hit different banks.
+    // A: rows of 128 bytes (four blocks of 16 columns), blocks XOR-swizzled by
+    // row so that the rows of one read hit different banks.
     int32_t ka[C::NA], oa[C::NA];
 #pragma unroll
     for (int j = 0; j < C::NA; ++j) {
-      const int b = (8 * j + wv) * 1024 + lane * 16, blk = b / C::AB, p = b % C::AB / 32, c = blk * 16 % rp + b % 32 / 2;
+      const int k = (8 * j + wv) * 8 + lane / 8, blk = (lane % 8 / 2) ^ swz<false>(k), c = blk * 16 % rp + lane % 2 * 8;
       int own = id[0];
 #pragma unroll
       for (int i = 1; i < SH_NB; ++i) own = blk == i ? id[i] : own;
-      ka[j] = p ^ (((p >> 3) & 1) << 2);
-      oa[j] = own >= 0 && c < R ? ka[j] * lda + (own * R + c) * 2 : INT32_MIN;
+      ka[j] = k;
+      oa[j] = own >= 0 && c < R ? k * lda + (own * R + c) * 2 : INT32_MIN;
     }
-    auto issue = [&](int s) {
-      char* st = ring + (s - s_lo) % C::RING * C::STEP;
+    auto issue_x = [&](int s) {
       const int k0 = s * C::KS, left = s < s_hi ? d_in - k0 : 0;
-      lds_dma16(rx, st + wv * 1024, kx < left && ox != INT32_MIN ? ox + k0 * E : INT32_MIN, 0);
+      lds_dma16(rx, ring + (s - s_lo) % C::RING * C::STEP + wv * 1024, kx < left && ox != INT32_MIN ? ox + k0 * E : INT32_MIN, 0);
+    };
+    auto issue_a = [&](int s) {
+      const int k0 = s * C::KS, left = s < s_hi ? d_in - k0 : 0;
 #pragma unroll
       for (int j = 0; j < C::NA; ++j)
-        lds_dma16(ra, st + C::XB + (8 * j + wv) * 1024,
+        lds_dma16(ra, ring + (s - s_lo) % C::RING * C::STEP + C::XB + (8 * j + wv) * 1024,
                   ka[j] < left && oa[j] != INT32_MIN ? (int32_t)((uint32_t)oa[j] + (uint32_t)k0 * (uint32_t)lda) : INT32_MIN, 0);
     };
     // This wave's rows 16 tb .. and blocks cb and cb + 2.
     const int tb = wv & 3, cb = wv >> 2, row = 16 * tb + c16, xs = (row >> 1) & 7;
     f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     __syncthreads();  // the stages of the agents before are read
-    for (int i = 0; i < C::RING - 1; ++i) issue(s_lo + i);
+    for (int i = 0; i < C::RING - 1; ++i) issue_x(s_lo + i);
+    for (int i = 0; i < C::RING - 1; ++i) issue_a(s_lo + i);
     for (int s = s_lo; s < s_hi; ++s) {
-      wait_loads<(C::RING - 2) * C::NI>();
+      wait_loads<(C::RING - 2) * C::NA>();  // no more come after stage s, from the first stage to the last
       wait_lds();
       __builtin_amdgcn_s_barrier();  // stage s has landed, stage s - 1 is read
       asm volatile("" ::: "memory");
-      issue(s + C::RING - 1);
+      issue_x(s + C::RING - 1);
+      issue_a(s + C::RING - 1);
       const char* st = ring + (s - s_lo) % C::RING * C::STEP;
 #pragma unroll
       for (int kk = 0; kk < C::KS / 32; ++kk) {
@@ -434,10 +438,9 @@ __global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ks
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           if (id[cb + 2 * i] < 0) continue;  // uniform
-          const int r = 8 * q + c16 / 4;
-          const char* p = st + C::XB + (cb + 2 * i) * C::AB + (32 * kk + (r ^ (((r >> 3) & 1) << 2))) * 32 + c16 % 4 * 8;
-          const char* p4 = st + C::XB + (cb + 2 * i) * C::AB + (32 * kk + ((r + 4) ^ (((r >> 3) & 1) << 2))) * 32 + c16 % 4 * 8;
-          const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p4);
+          const int r = 8 * q + c16 / 4;  // row r + 4 and those 32 further swizzle alike
+          const char* p = st + C::XB + (32 * kk + r) * 128 + ((cb + 2 * i) ^ swz<false>(r)) * 32 + c16 % 4 * 8;
+          const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 512);
           acc[i] = mfma16x16x32(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}), x, acc[i]);
         }
       }
@@ -533,69 +536,80 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
   // Agents of the tile's tokens (four or two a lane) and of this wave's.
   constexpr int NT = TT / 64;
   int all[NT], ag[TB];
-  bool any = false;
+  uint64_t todo[NT], any = 0;  // tokens whose agent is still to come, the same in every wave
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int64_t t = t0 + 64 * i + lane;
     all[i] = t < a.T ? a.agent[t] : -1;
-    any = any || (all[i] >= 0 && all[i] < a.n_agents);
+    todo[i] = __ballot(all[i] >= 0 && all[i] < a.n_agents);
+    any |= todo[i];
   }
-  if (__ballot(any) == 0) return;  // the same in every wave
+  if (any == 0) return;
 #pragma unroll
   for (int tb = 0; tb < TB; ++tb) ag[tb] = t0 + tw + 32 * tb + l32 < a.T ? a.agent[t0 + tw + 32 * tb + l32] : -1;
   auto chunk = [&](int r, int c) {  // where chunk c of row r lies
     return r * rp * 2 + (nc == 2 ? c : (nc == 4 ? c ^ ((r >> 2) & 3) : c ^ ((r >> 1) & 7))) * 16;
   };
-  {
-    // Thread tid: 1 / TPT of row tid / TPT.
-    constexpr int TPT = 512 / TT;
-    const int r = tid / TPT;
-    const int64_t t = t0 + r;
-    const int own = t < a.T ? a.agent[t] : -1;
-    const bool ok = own >= 0 && own < a.n_agents;
-    const float* H = static_cast<const float*>(a.ws) + t * R;
-    const float xsc = FP8 && ok ? a.x_scale[t] : 1.f;
-    for (int c = tid % TPT; c < nc; c += TPT) {
-      f32x4 v0 = {0.f, 0.f, 0.f, 0.f}, v1 = {0.f, 0.f, 0.f, 0.f};
-      if (ok && c * 8 < R)
-        for (int k = 0; k < ksa; ++k) {
-          const f32x4* p = reinterpret_cast<const f32x4*>(H + k * a.T * R + c * 8);
-          v0 += p[0];
-          v1 += p[1];
-        }
-      if constexpr (FP8) {
-        v0 *= xsc;
-        v1 *= xsc;
+  auto rows_to_lds = [&]() {
+    // 16-byte chunk u of the tile's rows is thread u % 512's, two at a time.
+    const float* H = static_cast<const float*>(a.ws) + t0 * R;
+    for (int u0 = tid; u0 < TT * nc; u0 += 1024) {
+      f32x4 v[2][2];
+      bool ok[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int u = u0 + 512 * i, r = u / nc;
+        const int own = u < TT * nc && t0 + r < a.T ? a.agent[t0 + r] : -1;
+        ok[i] = own >= 0 && own < a.n_agents && u % nc * 8 < R;
+        v[i][0] = v[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
-      *reinterpret_cast<u32x4*>(lds + chunk(r, c)) =
-          u32x4{pack_bf16(v0[0], v0[1]), pack_bf16(v0[2], v0[3]), pack_bf16(v1[0], v1[1]), pack_bf16(v1[2], v1[3])};
+#pragma unroll 4
+      for (int k = 0; k < ksa; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (ok[i]) {
+            const int u = u0 + 512 * i;
+            const f32x4* p = reinterpret_cast<const f32x4*>(H + k * a.T * R + (u / nc) * R + u % nc * 8);
+            v[i][0] += p[0];
+            v[i][1] += p[1];
+          }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int u = u0 + 512 * i;
+        if (u >= TT * nc) break;
+        if constexpr (FP8) {
+          const float xsc = ok[i] ? a.x_scale[t0 + u / nc] : 1.f;
+          v[i][0] *= xsc;
+          v[i][1] *= xsc;
+        }
+        *reinterpret_cast<u32x4*>(lds + chunk(u / nc, u % nc)) =
+            u32x4{pack_bf16(v[i][0][0], v[i][0][1]), pack_bf16(v[i][0][2], v[i][0][3]), pack_bf16(v[i][1][0], v[i][1][1]),
+                  pack_bf16(v[i][1][2], v[i][1][3])};
+      }
     }
-  }
+  };
   constexpr int WRB = NP * 64;  // bytes of a row of B
   char* bs = lds + TT * rp * 2;
   const int wk = 8 * h + i16 / 4, ws = swz_blocks<false, NP>(wk);
   const int wo = wk * WRB + (grp & 1) * 32 + i16 % 4 * 8;
-  int last = -1;
-  while (true) {
-    // The next agents in ascending order: the least above `last`, four times.
+  for (bool first = true; any != 0; first = false) {
     int id[EX_A];
 #pragma unroll
     for (int g = 0; g < EX_A; ++g) {
-      int m = INT32_MAX;
+      id[g] = -1;
 #pragma unroll
-      for (int i = 0; i < NT; ++i) m = all[i] > last && all[i] < a.n_agents && all[i] < m ? all[i] : m;
+      for (int i = NT - 1; i >= 0; --i)
+        if (todo[i] != 0) id[g] = __builtin_amdgcn_readlane(all[i], __builtin_ctzll(todo[i]));
+      any = 0;
 #pragma unroll
-      for (int x = 1; x < 64; x *= 2) {
-        const int o = __shfl_xor(m, x, kWave);
-        m = o < m ? o : m;
+      for (int i = 0; i < NT; ++i) {
+        todo[i] &= ~__ballot(all[i] == id[g]);
+        any |= todo[i];
       }
-      id[g] = __builtin_amdgcn_readfirstlane(m);
-      if (id[g] != INT32_MAX) last = id[g];
     }
-    if (id[0] == INT32_MAX) break;
 #pragma unroll
     for (int g = 0; g < EX_A; ++g) {
-      if (id[g] == INT32_MAX) break;
+      if (id[g] < 0) break;
       const i32x4 rb = buffer_rsrc(a.B + (int64_t)id[g] * R * a.d_out, (int32_t)(R * a.d_out * 2));
       for (int i = wv; i < rp * NP / 16; i += 8) {
         const int b = i * 1024 + lane * 16, k = b / WRB, p = b % WRB / 64, in = b % 64 / 2;
@@ -603,11 +617,12 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
         lds_dma16(rb, bs + g * rp * WRB + i * 1024, k < R && col < a.d_out ? (int32_t)((k * a.d_out + col) * 2) : INT32_MIN, 0);
       }
     }
+    if (first) rows_to_lds();
     wait_loads<0>();
-    __syncthreads();  // rows and agents are in LDS
+    __syncthreads();  // the rows and these agents are in LDS
 #pragma unroll
     for (int g = 0; g < EX_A; ++g) {
-      if (id[g] == INT32_MAX) break;
+      if (id[g] < 0) break;
 #pragma unroll
       for (int tb = 0; tb < TB; ++tb) {
         const bool mine = ag[tb] == id[g];
