@@ -350,6 +350,7 @@ hipError_t launch_stream(const ProjectArgs& a, hipStream_t st) {
 // A's rows are short (2 r bytes, and a CU takes one request of up to 128 bytes
 // every other cycle), so A bounds it: 64 rows a workgroup share each of them.
 constexpr int SH_T = 64, SH_NB = 4;  // rows; 16-column blocks
+constexpr int SH_TURNS = 2;
 
 template <bool FP8>
 struct Shrink {
@@ -362,7 +363,7 @@ struct Shrink {
 
 template <bool FP8>
 __global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ksa) {
-  using C = Shrink<FP8>;
+  using C = Shrink<FP8>;  // workgroup (ki + ksa * rows, turn)
   constexpr int E = C::E;
   __shared__ __attribute__((aligned(1024))) char ring[C::RING * C::STEP];
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, c16 = lane & 15;
@@ -380,7 +381,7 @@ __global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ks
   // X: rows 8 wv .. of this wave, 16-byte chunks XOR-swizzled by row.
   const int xr = 8 * wv + lane / 8, kx = ((lane % 8) ^ ((xr >> 1) & 7)) * 16 / E;
   const int32_t ox = xr < toks ? xr * ldx + kx * E : INT32_MIN;
-  while (todo != 0) {
+  for (int turn = 0; todo != 0; ++turn) {
     // The agents of blocks 0 .. 3 (-1: none).
     int id[SH_NB];
 #pragma unroll
@@ -392,6 +393,8 @@ __global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ks
       id[b] = todo != 0 ? __builtin_amdgcn_readlane(ag, __builtin_ctzll(todo)) : -1;
       if (todo != 0) todo &= ~__ballot(ag == id[b]);
     }
+    // Rows with more agents than that take turns, SH_TURNS workgroups at once.
+    if (turn % SH_TURNS != (int)blockIdx.y) continue;  // uniform
     // A: rows of 128 bytes (four blocks of 16 columns), blocks XOR-swizzled by
     // row so that the rows of one read hit different banks.
     int32_t ka[C::NA], oa[C::NA];
@@ -422,7 +425,9 @@ __global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ks
     for (int i = 0; i < C::RING - 1; ++i) issue_x(s_lo + i);
     for (int i = 0; i < C::RING - 1; ++i) issue_a(s_lo + i);
     for (int s = s_lo; s < s_hi; ++s) {
-      wait_loads<(C::RING - 2) * C::NA>();  // no more come after stage s, from the first stage to the last
+      // After stage s came the A of the RING - 2 first stages, or both of as many.
+      if (s < s_lo + C::RING - 1) wait_loads<(C::RING - 2) * C::NA>();
+      else wait_loads<(C::RING - 2) * C::NI>();
       wait_lds();
       __builtin_amdgcn_s_barrier();  // stage s has landed, stage s - 1 is read
       asm volatile("" ::: "memory");
@@ -455,12 +460,13 @@ __global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ks
   }
 }
 
-// k slices of the adapter rows: enough workgroups for the CUs, at most 8, two
-// stages each at least.
-int shrink_slices(int64_t T, int64_t d_in, int cus) {
-  const int64_t rows = (T + SH_T - 1) / SH_T, most = d_in / 256;
+// k slices of the adapter rows: enough workgroups for the CUs, two stages each at
+// least; no more than 256 sums a row, which every tile of the row adds.
+int shrink_slices(int64_t T, int64_t d_in, int rank, int cus) {
+  const int64_t rows = (T + SH_T - 1) / SH_T, most = d_in / 256, sums = 256 / rank;
   int64_t k = cus / rows;
   k = k > most ? most : k;
+  k = k > sums ? sums : k;
   return (int)(k < 1 ? 1 : (k > 8 ? 8 : k));
 }
 
@@ -518,10 +524,9 @@ __device__ __forceinline__ void scale_tile(const ProjectArgs& a, f32x16 (&acc)[C
 // The expanded adapter rows: all waves of the tile (TT tokens from t0, NP column
 // blocks from c0) together, four of its agents at a time.  The tile's rows X A_a
 // are summed over the k slices, rounded to bf16 and put into LDS, and each
-// agent's rows of B_a beside them, laid out as the weights are.  Where a block
-// of 32 tokens has one agent (tokens past T go with any) its product is summed
-// in place; else it is added to that agent's tokens alone, so that what is
-// infinite or NaN in an adapter stays in the rows that use it.
+// agent's rows of B_a beside them, laid out as the weights are.  A product
+// is added to the tokens of its agent alone, so that what is infinite
+// or NaN in an adapter stays in the rows that use it.
 constexpr int EX_A = 4;  // agents at a time
 
 template <int NP, int TT>
@@ -623,27 +628,73 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
 #pragma unroll
     for (int g = 0; g < EX_A; ++g) {
       if (id[g] < 0) break;
+      if constexpr (CB * TB >= 8) {
+        // 128 sums a lane leave room for one block's fragments at a time (more
+        // spills: 34 us against 23 at 4096 x 256 x 4096).
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) {
+          const bool mine = ag[tb] == id[g];
+          if (__ballot(mine) == 0) continue;
+          const bool whole = __ballot(mine || t0 + tw + 32 * tb + l32 >= a.T) == ~0ull;
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) {
+            f32x16 sum;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum[j] = whole ? acc[cb][tb][j] : 0.f;
+            for (int kk = 0; kk < rp / 16; ++kk) {
+              const char* p = bs + g * rp * WRB + wo + ((cb0 + cb) ^ ws) * 64 + 16 * kk * WRB;
+              const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * WRB);
+              u32x4 fh = *reinterpret_cast<const u32x4*>(lds + chunk(tw + 32 * tb + l32, 2 * kk + h));
+              if (!mine) fh = u32x4{0u, 0u, 0u, 0u};
+              sum = mfma32x32x16(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}), as_bf16x8(fh), sum);
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[cb][tb][j] = whole ? sum[j] : (mine ? acc[cb][tb][j] + sum[j] : acc[cb][tb][j]);
+          }
+        }
+        continue;
+      }
+      bool mine[TB];
+      uint64_t some = 0;
 #pragma unroll
       for (int tb = 0; tb < TB; ++tb) {
-        const bool mine = ag[tb] == id[g];
-        if (__ballot(mine) == 0) continue;
-        const bool whole = __ballot(mine || t0 + tw + 32 * tb + l32 >= a.T) == ~0ull;
+        mine[tb] = ag[tb] == id[g];
+        some |= __ballot(mine[tb]);
+      }
+      if (some == 0) continue;  // uniform
+      auto add = [&](auto KR) {  // KR steps of 16 ranks
+        constexpr int kr = decltype(KR)::value;
+        bf16x8 fh[TB][kr];
+#pragma unroll
+        for (int kk = 0; kk < kr; ++kk)
+#pragma unroll
+          for (int tb = 0; tb < TB; ++tb)
+            fh[tb][kk] = as_bf16x8(*reinterpret_cast<const u32x4*>(lds + chunk(tw + 32 * tb + l32, 2 * kk + h)));
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-          f32x16 sum;
+          const char* p = bs + g * rp * WRB + wo + ((cb0 + cb) ^ ws) * 64;
+          bf16x8 fb[kr];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) sum[j] = whole ? acc[cb][tb][j] : 0.f;
-          for (int kk = 0; kk < rp / 16; ++kk) {
-            const char* p = bs + g * rp * WRB + wo + ((cb0 + cb) ^ ws) * 64 + 16 * kk * WRB;
-            const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * WRB);
-            u32x4 fh = *reinterpret_cast<const u32x4*>(lds + chunk(tw + 32 * tb + l32, 2 * kk + h));
-            if (!mine) fh = u32x4{0u, 0u, 0u, 0u};
-            sum = mfma32x32x16(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}), as_bf16x8(fh), sum);
+          for (int kk = 0; kk < kr; ++kk) {
+            const u32x2 lo = lds_read_tr16(p + 16 * kk * WRB), hi = lds_read_tr16(p + (16 * kk + 4) * WRB);
+            fb[kk] = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
           }
 #pragma unroll
-          for (int j = 0; j < 16; ++j) acc[cb][tb][j] = whole ? sum[j] : (mine ? acc[cb][tb][j] + sum[j] : acc[cb][tb][j]);
+          for (int tb = 0; tb < TB; ++tb) {
+            f32x16 sum;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum[j] = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < kr; ++kk) sum = mfma32x32x16(fb[kk], fh[tb][kk], sum);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[cb][tb][j] += mine[tb] ? sum[j] : 0.f;
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-      }
+      };
+      if (rp == 16) add(std::integral_constant<int, 1>{});
+      else if (rp == 32) add(std::integral_constant<int, 2>{});
+      else add(std::integral_constant<int, 4>{});
     }
     __syncthreads();  // all is read
   }
@@ -1136,9 +1187,9 @@ hipError_t launch_mid(const ProjectArgs& a, int ksa, hipStream_t st) {
 template <bool FP8>
 hipError_t launch(const ProjectArgs& a, hipStream_t st) {
   if (a.T <= ST_T) return launch_stream<FP8>(a, st);
-  const int ksa = shrink_slices(a.T, a.d_in, a.cus);
+  const int ksa = shrink_slices(a.T, a.d_in, a.rank, a.cus);
   if (a.n_agents > 0) {
-    hipLaunchKernelGGL((shrink_kernel<FP8>), dim3((unsigned)((a.T + SH_T - 1) / SH_T * ksa)), dim3(512), 0, st, a, ksa);
+    hipLaunchKernelGGL((shrink_kernel<FP8>), dim3((unsigned)((a.T + SH_T - 1) / SH_T * ksa), SH_TURNS), dim3(512), 0, st, a, ksa);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   // The width that takes the least time by rounds of the CUs.
@@ -1172,7 +1223,7 @@ size_t adapted_projection_bytes(int64_t T, int64_t d_in, int64_t d_out, int n_ag
     const size_t b = stream_bytes(T, d_out, rank, stream_plan(T, d_in, d_out, n_agents, rank, true, cus));
     return a > b ? a : b;
   }
-  return n_agents > 0 ? (size_t)shrink_slices(T, d_in, cus) * (size_t)T * (size_t)rank * 4 : 0;
+  return n_agents > 0 ? (size_t)shrink_slices(T, d_in, rank, cus) * (size_t)T * (size_t)rank * 4 : 0;
 }
 
 hipError_t launch_adapted_projection(const ProjectArgs& a, hipStream_t st) {
