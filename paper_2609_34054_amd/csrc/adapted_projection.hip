@@ -8,7 +8,6 @@
 #include "kernels.hpp"
 
 #include <type_traits>
-#include <cstdlib>
 
 namespace prc {
 namespace {
@@ -1184,6 +1183,38 @@ hipError_t launch_mid(const ProjectArgs& a, int ksa, hipStream_t st) {
   return hipGetLastError();
 }
 
+// The tile shape that takes the least time.  A CU holds one tile at a time, so a
+// launch takes as many rounds as its tiles fill the CUs; a round takes a fixed
+// time and one that goes with d_in (microseconds, the latter at 4096), less in a
+// round that leaves CUs idle (down to about 0.6 of it: the clock rises), and
+// more where adapter rows are added.  Measured with 256 tiles at d_in 1024 and
+// 4096, bf16 and e4m3.
+int tile_form(const ProjectArgs& a, bool fp8) {
+  struct Form {
+    int toks, cols;
+    double fixed[2], per[2], lr;
+  };
+  static constexpr Form forms[6] = {
+      {128, 64, {4.8, 4.9}, {20.0, 12.3}, 3.0},    {128, 128, {6.7, 6.9}, {29.2, 14.1}, 3.0},
+      {256, 128, {6.1, 8.0}, {55.8, 28.1}, 6.0},   {256, 160, {6.2, 8.4}, {73.3, 31.9}, 6.0},
+      {256, 192, {6.9, 8.9}, {78.3, 36.4}, 6.0},   {256, 256, {7.6, 11.6}, {105.0, 46.4}, 6.0},
+  };
+  int best = 0;
+  double least = 1e300;
+  for (int i = 0; i < 6; ++i) {
+    const Form& f = forms[i];
+    const int64_t tiles = ((a.T + f.toks - 1) / f.toks) * ((a.d_out + f.cols - 1) / f.cols), rounds = tiles / a.cus,
+                  rest = tiles % a.cus;
+    const double fixed = f.fixed[fp8] + (a.n_agents > 0 ? f.lr : 0.0), per = f.per[fp8] * (double)a.d_in / 4096.0;
+    const double t = (double)rounds * (fixed + per) + (rest > 0 ? fixed + per * (0.6 + 0.4 * (double)rest / a.cus) : 0.0);
+    if (t < least) {
+      least = t;
+      best = i;
+    }
+  }
+  return best;
+}
+
 template <bool FP8>
 hipError_t launch(const ProjectArgs& a, hipStream_t st) {
   if (a.T <= ST_T) return launch_stream<FP8>(a, st);
@@ -1192,25 +1223,13 @@ hipError_t launch(const ProjectArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((shrink_kernel<FP8>), dim3((unsigned)((a.T + SH_T - 1) / SH_T * ksa), SH_TURNS), dim3(512), 0, st, a, ksa);
     if (const hipError_t e = hipGetLastError()) return e;
   }
-  // The width that takes the least time by rounds of the CUs.
-  int best = 8;
-  double least = 1e300;
-  for (int np : {8, 6, 5, 4}) {
-    const int64_t tiles = ((a.T + TL_T - 1) / TL_T) * ((a.d_out + 32 * np - 1) / (32 * np));
-    const double t = (double)((tiles + a.cus - 1) / a.cus) * (np + 0.5);
-    if (t < least) {
-      least = t;
-      best = np;
-    }
-  }
-  if (const char* f = getenv("TL_NP")) best = atoi(f);
-  switch (best) {
-    case 8: return launch_tiles<FP8, 4, 4>(a, ksa, st);
-    case 6: return launch_tiles<FP8, 3, 3>(a, ksa, st);
-    case 5: return launch_tiles<FP8, 3, 2>(a, ksa, st);
-    case 14: return launch_mid<FP8, 4>(a, ksa, st);
-    case 12: return launch_mid<FP8, 2>(a, ksa, st);
-    default: return launch_tiles<FP8, 2, 2>(a, ksa, st);
+  switch (tile_form(a, FP8)) {
+    case 0: return launch_mid<FP8, 2>(a, ksa, st);
+    case 1: return launch_mid<FP8, 4>(a, ksa, st);
+    case 2: return launch_tiles<FP8, 2, 2>(a, ksa, st);
+    case 3: return launch_tiles<FP8, 3, 2>(a, ksa, st);
+    case 4: return launch_tiles<FP8, 3, 3>(a, ksa, st);
+    default: return launch_tiles<FP8, 4, 4>(a, ksa, st);
   }
 }
 
