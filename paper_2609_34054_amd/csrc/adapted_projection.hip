@@ -83,7 +83,9 @@ struct Stream {
   static constexpr int CW = FP8 ? 128 : 64, NB = CW / 16;     // columns and 16-column blocks of a tile
   static constexpr int XI = FP8 ? (TB + 1) / 2 : TB;          // 1 KB loads of X per step
   static constexpr int NI = 4 + XI, STEP = NI * 1024;         // loads and bytes of a step
-  static constexpr int RING = 20 / NI;                        // steps in flight: 16 to 20 KB a wave
+  // Steps in flight: 10 KB a wave for up to 16 rows, so that a CU holds two
+  // workgroups and those of the adapters run beside the others'; else 16 to 18.
+  static constexpr int PER_CU = TB == 1 ? 2 : 1, RING = 20 / PER_CU / NI;
   static constexpr int G = NB * TB > 16 ? 16 / TB : NB;       // column blocks summed at a time (LDS)
   static_assert(ST_W * G * TB * 1024 <= ST_W * RING * STEP, "partials fit the ring");
   static_assert(ST_W * RING * STEP <= 160 * 1024, "LDS");
@@ -253,39 +255,38 @@ __global__ void __launch_bounds__(ST_W * 64) stream_kernel(const ProjectArgs a, 
   });
 }
 
-// Y of 256 columns of a row: a wave, four columns a lane.
+// Y of 256 columns of a row, four columns a lane: each of four waves takes a
+// quarter of the ranks and every fourth k slice, all its loads in flight at once
+// (lanes past the last column read the row's first ones); their sums are added
+// in a fixed order.
 template <int R>
-__global__ void __launch_bounds__(64) join_kernel(const ProjectArgs a, const StreamPlan p) {
-  const int lane = threadIdx.x;
-  const int64_t t = blockIdx.y, c = (int64_t)blockIdx.x * 256 + lane * 4, T = a.T;
+__global__ void __launch_bounds__(256) join_kernel(const ProjectArgs a, const StreamPlan p) {
+  constexpr int RW = R / 4;
+  __shared__ f32x4 part[3][64];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t t = blockIdx.y, c0 = (int64_t)blockIdx.x * 256 + lane * 4, T = a.T;
   const float* P = static_cast<const float*>(a.ws);
-  const bool ok = c < a.d_out;
+  const bool ok = c0 < a.d_out;
+  const int64_t c = ok ? c0 : 0;
   const int ag = a.n_agents > 0 ? a.agent[t] : -1;
   const bool lr = ag >= 0 && ag < a.n_agents;  // uniform
   const float xs = a.x_scale != nullptr ? a.x_scale[t] : 1.f;
+  f32x4 wsc = {1.f, 1.f, 1.f, 1.f};
+  if (a.x_scale != nullptr) wsc = *reinterpret_cast<const f32x4*>(a.w_scale + c) * xs;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  u32x2 b[R];
-  float h = 0.f;
+  for (int k = w; k < p.ks; k += 4) v += *reinterpret_cast<const f32x4*>(P + (k * T + t) * a.d_out + c);
+  v *= wsc;
   if (lr) {
-    const uint16_t* B = a.B + (int64_t)ag * R * a.d_out + c;
+    u32x2 b[RW];
+    const uint16_t* B = a.B + ((int64_t)ag * R + w * RW) * a.d_out + c;
 #pragma unroll
-    for (int j = 0; j < R; ++j) b[j] = ld8(B + j * a.d_out, ok);
-    const float* H = P + p.ks * T * a.d_out + t * R;
-    if (lane < R)
-      for (int k = 0; k < p.ksa; ++k) h += H[k * T * R + lane];
-  }
-  if (ok) {
-    for (int k = 0; k < p.ks; ++k) v += *reinterpret_cast<const f32x4*>(P + (k * T + t) * a.d_out + c);
-    if (a.x_scale != nullptr) {
-      const f32x4 wsc = *reinterpret_cast<const f32x4*>(a.w_scale + c);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] *= xs * wsc[i];
-    }
-  }
-  if (lr) {
+    for (int j = 0; j < RW; ++j) b[j] = *reinterpret_cast<const u32x2*>(B + j * a.d_out);
+    const float* H = P + p.ks * T * a.d_out + t * R + w * RW + lane % RW;
+    float h = 0.f;
+    for (int k = 0; k < p.ksa; ++k) h += H[k * T * R];
     const float hb = bf_lo(pack_bf16(h * xs, 0.f));
 #pragma unroll
-    for (int j = 0; j < R; ++j) {
+    for (int j = 0; j < RW; ++j) {
       const float hj = readlane_f(hb, j);
       v[0] += hj * bf_lo(b[j][0]);
       v[1] += hj * bf_hi(b[j][0]);
@@ -293,11 +294,18 @@ __global__ void __launch_bounds__(64) join_kernel(const ProjectArgs a, const Str
       v[3] += hj * bf_hi(b[j][1]);
     }
   }
-  if (ok) *reinterpret_cast<u32x2*>(a.Y + t * a.ld_y + c) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  if (w > 0) part[w - 1][lane] = v;
+  __syncthreads();
+  if (w > 0 || !ok) return;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) v += part[i][lane];
+  *reinterpret_cast<u32x2*>(a.Y + t * a.ld_y + c) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
 }
 
-// Column tiles, and k slices so that all workgroups of W and of the adapters
-// (each no longer than one of W) run at once, one a CU.
+// Column tiles, and k slices so that all workgroups run at once: those of W one
+// a CU, those of the adapters (as long as W's at most) beside them.  Up to 4 rows
+// two a CU (4096 x 4096: 11.3 us against 12.3 for one row, 15.2 against 13.5 for
+// 16: the slices' sums are written and read again).
 StreamPlan stream_plan(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, bool fp8, int cus) {
   StreamPlan p;
   const int cw = fp8 ? 128 : 64, ad = (int)(T < n_agents ? T : n_agents);
@@ -305,11 +313,11 @@ StreamPlan stream_plan(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int
   const int64_t steps = (d_in + 31) / 32;
   int most = (int)(steps / ST_W);  // a step a wave at least
   if (most < 1) most = 1;
-  p.ks = cus / p.n_ct;
+  p.ks = (T <= 4 ? 2 * cus : cus) / p.n_ct;
   p.ks = p.ks < 1 ? 1 : (p.ks > most ? most : p.ks);
-  auto slices = [&](int ks) { return (ks * rank + 63) / 64; };
-  while (p.ks > 1 && p.n_ct * p.ks + ad * slices(p.ks) > cus) --p.ks;
-  p.ksa = ad > 0 ? slices(p.ks) : 0;
+  const int slots = T <= 16 ? 2 * cus : cus;
+  while (p.ks > 1 && (p.n_ct + ad) * p.ks > slots) --p.ks;
+  p.ksa = ad > 0 ? p.ks : 0;
   return p;
 }
 size_t stream_bytes(int64_t T, int64_t d_out, int rank, const StreamPlan& p) {
@@ -331,10 +339,10 @@ hipError_t launch_stream(const ProjectArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)((a.d_out + 255) / 256), (unsigned)a.T);
   switch (a.rank) {
-    case 8: hipLaunchKernelGGL((join_kernel<8>), grid, dim3(64), 0, st, a, p); break;
-    case 16: hipLaunchKernelGGL((join_kernel<16>), grid, dim3(64), 0, st, a, p); break;
-    case 32: hipLaunchKernelGGL((join_kernel<32>), grid, dim3(64), 0, st, a, p); break;
-    default: hipLaunchKernelGGL((join_kernel<64>), grid, dim3(64), 0, st, a, p); break;
+    case 8: hipLaunchKernelGGL((join_kernel<8>), grid, dim3(256), 0, st, a, p); break;
+    case 16: hipLaunchKernelGGL((join_kernel<16>), grid, dim3(256), 0, st, a, p); break;
+    case 32: hipLaunchKernelGGL((join_kernel<32>), grid, dim3(256), 0, st, a, p); break;
+    default: hipLaunchKernelGGL((join_kernel<64>), grid, dim3(256), 0, st, a, p); break;
   }
   return hipGetLastError();
 }
