@@ -120,36 +120,53 @@ void rope_frequencies(double theta, int d, double* w2pi) {
 // stream).  A failed check launches nothing and returns PRC_EDEVDATA.
 int32_t* g_check_ptr[kMaxDevices];
 
-prc_status device_data_check(const char* who, const int32_t* positions, const int32_t* kv_len, int batch, int n_tok,
-                             int64_t s_cap, hipStream_t st) {
+prc_status check_array(const char* who, int32_t** res) {
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) {
     (void)hipGetLastError();
     return fail(PRC_EDEVICE, "no HIP device is current");
   }
-  int32_t* res = nullptr;
-  {
-    std::lock_guard<std::mutex> lk(g_dev_mu);
-    if (g_check_ptr[dev] == nullptr) {
-      int32_t* p = nullptr;
-      const hipError_t e = prc::device_checks_result(&p);
-      if (e != hipSuccess || p == nullptr) {
-        (void)hipGetLastError();
-        return fail(PRC_EDEVICE, "%s: device check array unavailable: %s", who, hipGetErrorString(e));
-      }
-      g_check_ptr[dev] = p;
+  std::lock_guard<std::mutex> lk(g_dev_mu);
+  if (g_check_ptr[dev] == nullptr) {
+    int32_t* p = nullptr;
+    const hipError_t e = prc::device_checks_result(&p);
+    if (e != hipSuccess || p == nullptr) {
+      (void)hipGetLastError();
+      return fail(PRC_EDEVICE, "%s: device check array unavailable: %s", who, hipGetErrorString(e));
     }
-    res = g_check_ptr[dev];
+    g_check_ptr[dev] = p;
   }
-  hipError_t e = prc::launch_device_checks(positions, kv_len, batch, n_tok, s_cap, res, st);
-  int32_t h[4] = {0, 0, 0, 0};
+  *res = g_check_ptr[dev];
+  return PRC_OK;
+}
+
+// Reads the verdict of the check launched with status e.
+prc_status read_check(const char* who, hipError_t e, const int32_t* res, hipStream_t st, int32_t (&h)[4]) {
   if (e == hipSuccess) e = hipMemcpyAsync(h, res, sizeof(h), hipMemcpyDeviceToHost, st);
   if (e == hipSuccess) e = hipStreamSynchronize(st);
   if (e != hipSuccess) return fail(PRC_ELAUNCH, "%s: device check failed: %s", who, hipGetErrorString(e));
+  return PRC_OK;
+}
+
+prc_status device_data_check(const char* who, const int32_t* positions, const int32_t* kv_len, int batch, int n_tok,
+                             int64_t s_cap, hipStream_t st) {
+  int32_t* res = nullptr;
+  if (prc_status s = check_array(who, &res)) return s;
+  int32_t h[4] = {0, 0, 0, 0};
+  if (prc_status s = read_check(who, prc::launch_device_checks(positions, kv_len, batch, n_tok, s_cap, res, st), res, st, h)) return s;
   if (h[0] == 1)
     return fail(PRC_EDEVDATA, "%s: kv_len[%d]=%d outside [1, s_cap=%lld]", who, h[1], h[3], (long long)s_cap);
   if (h[0] == 2)
     return fail(PRC_EDEVDATA, "%s: positions[%d][%d]=%d outside [0, kv_len[%d])", who, h[1], h[2], h[3], h[1]);
+  return PRC_OK;
+}
+
+prc_status agent_check(const char* who, const int32_t* agent, int64_t T, int n_agents, hipStream_t st) {
+  int32_t* res = nullptr;
+  if (prc_status s = check_array(who, &res)) return s;
+  int32_t h[4] = {0, 0, 0, 0};
+  if (prc_status s = read_check(who, prc::launch_agent_checks(agent, T, n_agents, res, st), res, st, h)) return s;
+  if (h[0] == 3) return fail(PRC_EDEVDATA, "%s: agent[%d]=%d is not below n_agents=%d", who, h[2], h[3], n_agents);
   return PRC_OK;
 }
 #endif
@@ -825,11 +842,13 @@ prc_status check_projection(int64_t T, int64_t d_in, int64_t d_out, int32_t n_ag
   if (T < 0 || T > INT32_MAX) return fail(PRC_EINVAL, "T=%lld outside [0, 2^31)", (long long)T);
   if (d_in < 1 || d_in % step || d_out < 1 || d_out % step)
     return fail(PRC_EUNSUPPORTED, "d_in=%lld, d_out=%lld must be positive multiples of %d", (long long)d_in, (long long)d_out, step);
+  if (d_out >= (1LL << 22) || T * d_out > (1LL << 42))
+    return fail(PRC_EUNSUPPORTED, "T=%lld rows of d_out=%lld are too many", (long long)T, (long long)d_out);
   if (n_agents < 0) return fail(PRC_EINVAL, "n_agents=%d is negative", n_agents);
   if (n_agents > 0 && !rank_ok(rank)) return fail(PRC_EUNSUPPORTED, "rank=%d (built: 8, 16, 32, 64)", rank);
   // Weights are addressed with 32-bit byte offsets.
   const int64_t most = (1LL << 30) - (1LL << 20);
-  if (d_in >= (1LL << 22) || d_out >= (1LL << 22) || d_in * d_out > most)
+  if (d_in >= (1LL << 22) || d_in * d_out > most)
     return fail(PRC_EUNSUPPORTED, "d_in=%lld times d_out=%lld weights are too many", (long long)d_in, (long long)d_out);
   if (n_agents > 0 && d_in * n_agents > most / rank)
     return fail(PRC_EUNSUPPORTED, "d_in=%lld times %d adapters of rank %d are too many", (long long)d_in, n_agents, rank);
@@ -897,6 +916,10 @@ prc_status adapted_impl(const char* who, const void* X, const float* x_scale, in
   int cus = 0;
   if (prc_status ds = device_ready(&cus)) return ds;
   a.cus = cus;
+#if PRC_DEVICE_CHECKS
+  if (lr)
+    if (prc_status dc = agent_check(who, agent, T, n_agents, stream)) return dc;
+#endif
   return launch_status(prc::launch_adapted_projection(a, stream), who);
 }
 
@@ -933,7 +956,8 @@ PRC_API prc_status adapted_projection_fp8(const uint8_t* X, const float* x_scale
 }
 
 PRC_API size_t adapted_projection_workspace_size(int64_t T, int64_t d_in, int64_t d_out, int32_t n_agents, int32_t rank) {
-  if (T < 1 || T > INT32_MAX || d_in < 1 || d_out < 1 || d_in >= (1LL << 22) || d_out >= (1LL << 22) || n_agents < 0 ||
+  if (T < 1 || T > INT32_MAX || d_in < 1 || d_out < 1 || d_in >= (1LL << 22) || d_out >= (1LL << 22) ||
+      T * d_out > (1LL << 42) || n_agents < 0 ||
       (n_agents > 0 && !rank_ok(rank)))
     return 0;
   return prc::adapted_projection_bytes(T, d_in, d_out, n_agents, rank, plan_cus());

@@ -1,5 +1,6 @@
 // Checks of the values the host cannot see, for the checked build of the
-// library (libprecache_checked.so): kv_len[b] must lie in [1, s_cap] and every
+// library (libprecache_checked.so): the agents of a projection's rows must lie
+// below n_agents, kv_len[b] must lie in [1, s_cap] and every
 // query position in [0, kv_len[b]) (the causal prefix of Sec. 2.2 is then
 // never empty and never reaches past the cache).  The release build trusts
 // these values; its kernels only clamp kv_len into [0, s_cap].
@@ -16,8 +17,9 @@ namespace {
 
 constexpr int DC_THREADS = 256;
 
-// result[0]: 0 all valid, 1 kv_len out of range, 2 position out of range;
-// result[1]: request; result[2]: query token; result[3]: the offending value.
+// result[0]: 0 all valid, 1 kv_len out of range, 2 position out of range, 3 agent
+// out of range; result[1]: request; result[2]: query token (agents: row);
+// result[3]: the offending value.
 static __device__ __align__(16) int32_t check_result[4];
 
 __global__ void __launch_bounds__(DC_THREADS)
@@ -55,7 +57,29 @@ device_checks_kernel(const int32_t* positions, const int32_t* kv_len, int batch,
   }
 }
 
+// The first row whose agent is at or past n_agents (negative: the base row).
+__global__ void __launch_bounds__(DC_THREADS) agent_checks_kernel(const int32_t* agent, int64_t T, int n_agents, int32_t* result) {
+  __shared__ long long first;
+  if (threadIdx.x == 0) first = LLONG_MAX;
+  __syncthreads();
+  for (int64_t i = threadIdx.x; i < T; i += DC_THREADS)
+    if (agent[i] >= n_agents) {
+      atomicMin(&first, (long long)i);
+      break;  // the later rows of this thread are no earlier
+    }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const bool bad = first != LLONG_MAX;
+    *reinterpret_cast<i32x4*>(result) = bad ? i32x4{3, 0, (int32_t)first, agent[first]} : i32x4{0, 0, 0, 0};
+  }
+}
+
 }  // namespace
+
+hipError_t launch_agent_checks(const int32_t* agent, int64_t T, int n_agents, int32_t* result, hipStream_t st) {
+  hipLaunchKernelGGL(agent_checks_kernel, dim3(1), dim3(DC_THREADS), 0, st, agent, T, n_agents, result);
+  return hipGetLastError();
+}
 
 hipError_t device_checks_result(int32_t** ptr) {
   void* p = nullptr;

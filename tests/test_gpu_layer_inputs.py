@@ -135,6 +135,34 @@ def test_projection_sizes(T, k, n, N, r, order, fp8):
     check_project(call(prc, c), *ref_of(c))
 
 
+# Sizes whose rounds of the CUs favour each of the tile shapes (128 x 64 to 256 x 256), with ends inside tiles.
+SHAPES_TILES = [(65, 272, 528), (1000, 1024, 4096), (2500, 1040, 2064), (2040, 272, 5120), (2040, 528, 6144),
+                (4090, 272, 4080), (3000, 528, 4096)]
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("N,r,order", [(3, 64, "some"), (9, 16, "runs"), (1, 32, "one"), (12, 8, "mixed"), (0, 0, "none")])
+@pytest.mark.parametrize("T,k,n", SHAPES_TILES)
+def test_projection_tile_shapes(T, k, n, N, r, order, fp8):
+    print(f"project {T} {k} {n} {N} r{r} {order} fp8={fp8}", flush=True)
+    c = project_case(T + k + n + r, T, k, n, N, r, order, fp8)
+    check_project(call(prc, c), *ref_of(c))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,k,n", SHAPES_TILES[1:6])
+def test_bad_adapters_stay_in_their_rows_of_wide_tiles(T, k, n, fp8):
+    for order, r in (("mixed", 16), ("runs", 64)):
+        c = project_case(T + r, T, k, n, 4, r, order, fp8)
+        want = call(prc, c)
+        bad = dict(c, B=c["B"].clone())
+        a = int(c["agent"][T // 2])
+        bad["B"][a, 5] = float("inf")
+        got = call(prc, bad)
+        mine = c["agent"] == a
+        assert torch.equal(got[~mine], want[~mine]) and (~torch.isfinite(got[mine].float())).all()
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("T", [1, 20, 130, 700])
 def test_projection_without_adapters(T, fp8):
@@ -305,3 +333,23 @@ def test_a_layers_input_to_attention():
     got = prc.adapted_projection_fp8(q8, qs, W8, w8s, A, Bq, agent)
     check_project(got, *ref_of({"X": q8, "x_scale": qs, "W": W8, "w_scale": w8s, "A_stack": A, "B": Bq, "agent": agent}))
     assert q8.dtype == E4M3 and norm_ref(o, w, s2, 1e-5)[0].shape == got.shape[:1] + (hid,)
+
+
+@pytest.mark.parametrize("T", [3, 700])
+def test_checked_library_reports_agents(T):
+    from paper_2609_34054_amd.binding import use_checked_library
+    c = project_case(4, T, 256, 272, 3, 16, "mixed")
+    want = call(prc, c)
+    c["agent"][1] = -7
+    base = call(prc, c)
+    try:
+        use_checked_library(True)
+        assert torch.equal(call(prc, c), base) and torch.equal(base[2:], want[2:])
+        c["agent"][2] = 3
+        with pytest.raises(prc.PrecacheError) as e:
+            call(prc, c)
+        assert e.value.status_name == "PRC_EDEVDATA" and "agent[2]=3" in str(e.value)
+    finally:
+        use_checked_library(False)
+    got = call(prc, c)
+    assert torch.equal(got[3:], want[3:]) and torch.isfinite(got.float()).all()

@@ -33,7 +33,8 @@ def _norm8(T=8, d=256, ldx=256, res=W, y=Y, ldy=256, ys=XS, out=B):
     (dict(n=12), EUNSUP), (dict(N=-1), EINVAL), (dict(r=12), EUNSUP), (dict(r=128), EUNSUP), (dict(r=0), EUNSUP),
     (dict(ldx=248), ESHAPE), (dict(ldy=504), ESHAPE), (dict(ldx=260), EALIGN), (dict(ldy=516), EALIGN),
     (dict(ldx=1 << 22), EUNSUP), (dict(ldy=1 << 22), EUNSUP), (dict(k=1 << 15, n=1 << 15), EUNSUP),
-    (dict(k=1 << 14, N=1 << 13, r=16), EUNSUP), (dict(X=None), EINVAL), (dict(W=None), EINVAL), (dict(A=None), EINVAL),
+    (dict(k=1 << 14, N=1 << 13, r=16), EUNSUP),
+    (dict(T=(1 << 31) - 1, k=8, n=1 << 12), EUNSUP), (dict(k=8, n=1 << 22), EUNSUP), (dict(k=1 << 22, n=8), EUNSUP), (dict(X=None), EINVAL), (dict(W=None), EINVAL), (dict(A=None), EINVAL),
     (dict(B=None), EINVAL), (dict(ag=None), EINVAL), (dict(Y=None), EINVAL), (dict(X=X + 8), EALIGN),
     (dict(W=W + 2), EALIGN), (dict(B=B + 8), EALIGN), (dict(Y=Y + 8), EALIGN), (dict(ag=AG + 2), EALIGN),
     (dict(ws=None), EWS), (dict(wb=16), EWS), (dict(ws=WS + 8), EALIGN), (dict(Y=X), EINVAL), (dict(Y=X + 16384), EINVAL),
