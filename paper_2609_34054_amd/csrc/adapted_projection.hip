@@ -441,21 +441,29 @@ __global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ks
       issue_x(s + C::RING - 1);
       issue_a(s + C::RING - 1);
       const char* st = ring + (s - s_lo) % C::RING * C::STEP;
+      // All of the stage's fragments, then its MFMAs (blocks without an agent are
+      // zeros): one wait a stage, not one a product.
+      constexpr int KK = C::KS / 32;
+      bf16x8 x[KK], w[KK][2];
 #pragma unroll
-      for (int kk = 0; kk < C::KS / 32; ++kk) {
-        bf16x8 x;
+      for (int kk = 0; kk < KK; ++kk) {
         const char* xp = st + row * 128;
-        if constexpr (FP8) x = as_bf16x8(bf16_of_e4m3(*reinterpret_cast<const u32x2*>(xp + ((2 * kk + q / 2) ^ xs) * 16 + q % 2 * 8)));
-        else x = as_bf16x8(*reinterpret_cast<const u32x4*>(xp + ((4 * kk + q) ^ xs) * 16));
+        if constexpr (FP8)
+          x[kk] = as_bf16x8(bf16_of_e4m3(*reinterpret_cast<const u32x2*>(xp + ((2 * kk + q / 2) ^ xs) * 16 + q % 2 * 8)));
+        else
+          x[kk] = as_bf16x8(*reinterpret_cast<const u32x4*>(xp + ((4 * kk + q) ^ xs) * 16));
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          if (id[cb + 2 * i] < 0) continue;  // uniform
           const int r = 8 * q + c16 / 4;  // row r + 4 and those 32 further swizzle alike
           const char* p = st + C::XB + (32 * kk + r) * 128 + ((cb + 2 * i) ^ swz<false>(r)) * 32 + c16 % 4 * 8;
           const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 512);
-          acc[i] = mfma16x16x32(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}), x, acc[i]);
+          w[kk][i] = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
         }
       }
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) acc[i] = mfma16x16x32(w[kk][i], x[kk], acc[i]);
     }
     wait_loads<0>();
     const int own = row < toks ? a.agent[t0 + row] : -1;
