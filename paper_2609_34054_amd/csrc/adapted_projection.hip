@@ -364,8 +364,10 @@ struct Shrink {
   static constexpr int E = FP8 ? 1 : 2, KS = 128 / E;          // bytes of an element; k of a stage
   static constexpr int XB = SH_T * 128, AB = KS * SH_NB * 32;  // bytes of X and of A
   static constexpr int NA = AB / 8192, NI = 1 + NA;            // a wave's loads of A, and all
-  static constexpr int STEP = XB + AB, RING = FP8 ? 6 : 8;
-  static_assert(RING * STEP <= 160 * 1024, "LDS");
+  // Two workgroups a CU: one's start and end beside the other's loads (4096 rows:
+  // 11.3 us against 14.1 with one and twice the stages).
+  static constexpr int STEP = XB + AB, RING = FP8 ? 3 : 5;
+  static_assert(RING * STEP <= 80 * 1024, "LDS");
 };
 
 template <bool FP8>
