@@ -12,24 +12,13 @@
 namespace prc {
 namespace {
 
+// LDS pointers that stay 32 bits wide, and accesses through them.
+typedef __attribute__((address_space(3))) char lds_char;
+__device__ __forceinline__ u32x4 lds_read16(const lds_char* p) { return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(p); }
 // Transposing LDS reads.  16-bit: lane j of a 16-lane group points at 4
 // elements, lane i receives element i % 4 of lanes i / 4, i / 4 + 4, ... + 12.
 // 8-bit: lane j points at 8 elements, lane i receives element i % 8 of lanes
 // i / 8, i / 8 + 2, ... + 14.
-__device__ __forceinline__ u32x2 lds_read_tr16(const void* p) {
-  typedef short v4s __attribute__((ext_vector_type(4)));
-  v4s v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s __attribute__((address_space(3)))*)(p));
-  return __builtin_bit_cast(u32x2, v);
-}
-__device__ __forceinline__ u32x2 lds_read_tr8(const void* p) {
-  typedef int v2i __attribute__((ext_vector_type(2)));
-  v2i v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((v2i __attribute__((address_space(3)))*)(p));
-  return __builtin_bit_cast(u32x2, v);
-}
-
-// LDS pointers that stay 32 bits wide, and accesses through them.
-typedef __attribute__((address_space(3))) char lds_char;
-__device__ __forceinline__ u32x4 lds_read16(const lds_char* p) { return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(p); }
 __device__ __forceinline__ u32x2 lds_tr16(const lds_char* p) {
   typedef short v4s __attribute__((ext_vector_type(4)));
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s __attribute__((address_space(3)))*)(p)));
@@ -38,6 +27,8 @@ __device__ __forceinline__ u32x2 lds_tr8(const lds_char* p) {
   typedef int v2i __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((v2i __attribute__((address_space(3)))*)(p)));
 }
+__device__ __forceinline__ u32x2 lds_read_tr16(const void* p) { return lds_tr16((const lds_char*)p); }
+__device__ __forceinline__ u32x2 lds_read_tr8(const void* p) { return lds_tr8((const lds_char*)p); }
 // lds_dma16 with the (wave-uniform) LDS address as a number.
 __device__ __forceinline__ void lds_dma16_at(i32x4 rsrc, uint32_t to, int32_t voff, int32_t soff) {
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(voff), "s"(rsrc), "s"(soff)
@@ -65,7 +56,7 @@ __device__ __forceinline__ u32x4 bf16_of_e4m3(u32x2 v) {
 }
 
 // ---------------------------------------------------------------------------
-// Few rows (T <= 64): the weights are streamed once, so memory bounds it.  A
+// Few rows (T <= 16): the weights are streamed once, so memory bounds it.  A
 // workgroup takes a column tile (128 bytes of each weight row) and a slice of
 // k, its eight waves an eighth of that each; a wave brings its own 32-k steps
 // (weights and the rows of X) through a private ring in LDS with direct loads,
@@ -75,20 +66,23 @@ __device__ __forceinline__ u32x4 bf16_of_e4m3(u32x2 v) {
 // the rows X A_a: a workgroup per distinct agent (and k slice).  The waves'
 // sums are added through LDS in a fixed order and go to the workspace; a
 // second kernel adds the k slices and the expanded adapter rows.
+//
+// 4096 x 4096 in bf16, one row: 11.9 us for both kernels, of which the weights
+// (32 MB) take 6.7 at the rate of a copy; the rest is two launches and the start
+// and end of the ring.  With more than 16 rows their loads and MFMAs, repeated
+// for each distinct agent, outweigh the barriers saved (see the slabs below).
 constexpr int ST_W = 8;   // waves
-constexpr int ST_T = 64;  // most rows
+constexpr int ST_T = 16;  // most rows
 
-template <bool FP8, int TB>  // TB blocks of 16 rows
+template <bool FP8>
 struct Stream {
-  static constexpr int CW = FP8 ? 128 : 64, NB = CW / 16;     // columns and 16-column blocks of a tile
-  static constexpr int XI = FP8 ? (TB + 1) / 2 : TB;          // 1 KB loads of X per step
-  static constexpr int NI = 4 + XI, STEP = NI * 1024;         // loads and bytes of a step
-  // Steps in flight: 10 KB a wave for up to 16 rows, so that a CU holds two
-  // workgroups and those of the adapters run beside the others'; else 16 to 18.
-  static constexpr int PER_CU = TB == 1 ? 2 : 1, RING = 20 / PER_CU / NI;
-  static constexpr int G = NB * TB > 16 ? 16 / TB : NB;       // column blocks summed at a time (LDS)
-  static_assert(ST_W * G * TB * 1024 <= ST_W * RING * STEP, "partials fit the ring");
-  static_assert(ST_W * RING * STEP <= 160 * 1024, "LDS");
+  static constexpr int CW = FP8 ? 128 : 64, NB = CW / 16;  // columns and 16-column blocks of a tile
+  static constexpr int NI = 5, STEP = NI * 1024;           // 1 KB loads (4 of weights, 1 of X) and bytes of a step
+  // Steps in flight: 10 KB a wave, so that a CU holds two workgroups and those
+  // of the adapters run beside the others'.
+  static constexpr int RING = 2;
+  static_assert(NB <= RING * NI, "partials fit the ring");
+  static_assert(ST_W * RING * STEP <= 80 * 1024, "LDS");
 };
 
 // Unit (16 columns) of weight row r is stored at unit ^ swz(r).
@@ -97,21 +91,21 @@ __device__ __forceinline__ int swz(int r) {
   return FP8 ? ((r >> 1) & 3) + 4 * ((r >> 3) & 1) : ((r >> 1) & 1) + 2 * ((r >> 3) & 1);
 }
 
-// One pass over this wave's steps [s_lo, s_hi): acc[nb][tb] += W^T X^T for the
+// One pass over this wave's steps [s_lo, s_hi): acc[nb] += W^T X^T for the
 // 16-column blocks nb.  AD: the weights are `rank` columns of A from column
 // col0 (bf16, NBA blocks), else a tile of W.
-template <bool FP8, int TB, bool AD, typename Acc>
-__device__ __forceinline__ void stream_steps(const ProjectArgs& a, char* ring, int64_t t0, int toks, int64_t col0, int s_lo,
-                                             int s_hi, Acc& acc) {
-  using C = Stream<FP8, TB>;
+template <bool FP8, bool AD>
+__device__ __forceinline__ void stream_steps(const ProjectArgs& a, char* ring, int toks, int64_t col0, int s_lo,
+                                             int s_hi, f32x4 (&acc)[Stream<FP8>::NB]) {
+  using C = Stream<FP8>;
   constexpr int XE = FP8 ? 1 : 2, WE = AD ? 2 : XE;  // bytes of an element
   const int lane = threadIdx.x & 63, q = lane >> 4, c16 = lane & 15;
   const int d_in = (int)a.d_in, R = a.rank;
   const int32_t ldw = (int32_t)((AD ? (int64_t)a.n_agents * R : a.d_out) * WE), ldx = (int32_t)(a.ld_x * XE);
   const i32x4 rw = buffer_rsrc(AD ? static_cast<const void*>(a.A) : a.W, d_in * ldw);
-  const i32x4 rx = buffer_rsrc(static_cast<const char*>(a.X) + t0 * ldx, (toks - 1) * ldx + d_in * XE);
+  const i32x4 rx = buffer_rsrc(a.X, (toks - 1) * ldx + d_in * XE);
   // Each lane's k within a step and byte offset at k = 0, for every load.
-  int32_t kw[4], ow[4], kx[C::XI], ox[C::XI];
+  int32_t kw[4], ow[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if constexpr (AD) {
@@ -125,12 +119,8 @@ __device__ __forceinline__ void stream_steps(const ProjectArgs& a, char* ring, i
       ow[j] = c < a.d_out ? kw[j] * ldw + (int32_t)c * WE : INT32_MIN;
     }
   }
-#pragma unroll
-  for (int j = 0; j < C::XI; ++j) {
-    const int t = FP8 ? j * 32 + lane / 2 : j * 16 + lane / 4;
-    kx[j] = FP8 ? lane % 2 * 16 : lane % 4 * 8;
-    ox[j] = t < toks && t < 16 * TB ? t * ldx + kx[j] * XE : INT32_MIN;
-  }
+  const int tx = FP8 ? lane / 2 : lane / 4, kx = FP8 ? lane % 2 * 16 : lane % 4 * 8;
+  const int32_t ox = tx < toks ? tx * ldx + kx * XE : INT32_MIN;
   auto issue = [&](int s) {
     char* st = ring + (s % C::RING) * C::STEP;
     const int k0 = s * 32;
@@ -138,9 +128,7 @@ __device__ __forceinline__ void stream_steps(const ProjectArgs& a, char* ring, i
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       lds_dma16(rw, st + j * 1024, kw[j] < left && ow[j] != INT32_MIN ? (int32_t)(ow[j] + (uint32_t)k0 * (uint32_t)ldw) : INT32_MIN, 0);
-#pragma unroll
-    for (int j = 0; j < C::XI; ++j)
-      lds_dma16(rx, st + 4096 + j * 1024, kx[j] < left && ox[j] != INT32_MIN ? ox[j] + k0 * XE : INT32_MIN, 0);
+    lds_dma16(rx, st + 4096, kx < left && ox != INT32_MIN ? ox + k0 * XE : INT32_MIN, 0);
   };
   for (int i = 0; i < C::RING; ++i) issue(s_lo + i);
   for (int s = s_lo; s < s_hi; ++s) {
@@ -148,34 +136,26 @@ __device__ __forceinline__ void stream_steps(const ProjectArgs& a, char* ring, i
     const char* st = ring + (s % C::RING) * C::STEP;
     const char* xp = st + 4096;
     if constexpr (FP8 && !AD) {
-      long x[TB];
-#pragma unroll
-      for (int tb = 0; tb < TB; ++tb) x[tb] = *reinterpret_cast<const long*>(xp + tb * 512 + c16 * 32 + q * 8);
+      const long x = *reinterpret_cast<const long*>(xp + c16 * 32 + q * 8);
       const int kr = 8 * q + c16 / 2;
 #pragma unroll
       for (int nb = 0; nb < C::NB; ++nb) {
         const long w = __builtin_bit_cast(long, lds_read_tr8(st + kr * 128 + (nb ^ swz<true>(kr)) * 16 + c16 % 2 * 8));
-#pragma unroll
-        for (int tb = 0; tb < TB; ++tb) acc[nb][tb] = __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(w, x[tb], acc[nb][tb], 0, 0, 0);
+        acc[nb] = __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(w, x, acc[nb], 0, 0, 0);
       }
     } else {
-      bf16x8 x[TB];
-#pragma unroll
-      for (int tb = 0; tb < TB; ++tb) {
-        if constexpr (FP8)
-          x[tb] = as_bf16x8(bf16_of_e4m3(*reinterpret_cast<const u32x2*>(xp + tb * 512 + c16 * 32 + q * 8)));
-        else
-          x[tb] = as_bf16x8(*reinterpret_cast<const u32x4*>(xp + tb * 1024 + c16 * 64 + q * 16));
-      }
+      bf16x8 x;
+      if constexpr (FP8)
+        x = as_bf16x8(bf16_of_e4m3(*reinterpret_cast<const u32x2*>(xp + c16 * 32 + q * 8)));
+      else
+        x = as_bf16x8(*reinterpret_cast<const u32x4*>(xp + c16 * 64 + q * 16));
       const int kr = 8 * q + c16 / 4, rb = AD ? 2 * R : 128;
 #pragma unroll
       for (int nb = 0; nb < 4; ++nb) {
         if (AD && nb * 16 >= R) break;  // uniform (rank 8: one block, its upper columns dropped)
         const char* p = st + kr * rb + (AD ? nb : nb ^ swz<false>(kr)) * 32 + c16 % 4 * 8;
         const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * rb);
-#pragma unroll
-        for (int tb = 0; tb < TB; ++tb)
-          acc[nb][tb] = mfma16x16x32(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}), x[tb], acc[nb][tb]);
+        acc[nb] = mfma16x16x32(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}), x, acc[nb]);
       }
     }
     wait_lds();  // this step's slot is free
@@ -184,56 +164,52 @@ __device__ __forceinline__ void stream_steps(const ProjectArgs& a, char* ring, i
   wait_loads<0>();
 }
 
-// Sums the waves' acc[g0 + g][tb] (g < n) through LDS in a fixed order and
-// hands out the sums of block g, row t, columns 4 q ..: put(g, t, q, sum).
-template <int TB, int G, int NB, typename Put>
-__device__ __forceinline__ void sum_waves(f32x4 (&acc)[NB][TB], char* lds, int g0, int n, Put put) {
+// Sums the waves' acc[g] (g < n <= G) through LDS in a fixed order and hands out
+// the sums of block g, row t, columns 4 q ..: put(g, t, q, sum).
+template <int G, int NB, typename Put>
+__device__ __forceinline__ void sum_waves(f32x4 (&acc)[NB], char* lds, int n, Put put) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  f32x4* part = reinterpret_cast<f32x4*>(lds);  // [wave][G][TB][64]
-  __syncthreads();  // the ring, or the sums before, are no longer read
+  f32x4* part = reinterpret_cast<f32x4*>(lds);  // [wave][G][64]
+  __syncthreads();  // the ring is no longer read
 #pragma unroll
-  for (int g = 0; g < G; ++g)
-#pragma unroll
-    for (int tb = 0; tb < TB; ++tb) part[((w * G + g) * TB + tb) * 64 + lane] = acc[g0 + g][tb];
+  for (int g = 0; g < G; ++g) part[(w * G + g) * 64 + lane] = acc[g];
   __syncthreads();
-  for (int u = tid; u < n * TB * 64; u += ST_W * 64) {
+  for (int u = tid; u < n * 64; u += ST_W * 64) {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < ST_W; ++v) s += part[v * G * TB * 64 + u];
-    put(u / (TB * 64), u / 64 % TB * 16 + u % 16, u / 16 % 4, s);
+    for (int v = 0; v < ST_W; ++v) s += part[v * G * 64 + u];
+    put(u / 64, u % 16, u / 16 % 4, s);
   }
 }
 
-// Workspace of the two kernels: sums of W [ks][T][d_out], then of the adapters
-// [ksa][T][rank], fp32.
-struct StreamPlan {
-  int n_ct, ks, ksa;
+// Workspace of a product over k slices: sums of W [ks][T][d_out], then of the
+// adapters [ksa][T][rank], fp32.
+struct SlabPlan {
+  int n_ct, n_tt, ks;  // column tiles of W (0: the adapter rows alone), row tiles, k slices
+  int ksa;             // k slices of the adapter rows (0: none)
+  int64_t h_at;        // fp32 words before their sums
 };
 
-template <bool FP8, int TB>
-__global__ void __launch_bounds__(ST_W * 64) stream_kernel(const ProjectArgs a, const StreamPlan p) {
-  using C = Stream<FP8, TB>;
+template <bool FP8>
+__global__ void __launch_bounds__(ST_W * 64) stream_kernel(const ProjectArgs a, const SlabPlan p) {
+  using C = Stream<FP8>;
   __shared__ __attribute__((aligned(1024))) char lds[ST_W * C::RING * C::STEP];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int T = (int)a.T, nk = (int)((a.d_in + 31) / 32);
   char* ring = lds + w * C::RING * C::STEP;
   const int n_main = p.n_ct * p.ks;
-  f32x4 acc[C::NB][TB];
+  f32x4 acc[C::NB];
 #pragma unroll
-  for (int i = 0; i < C::NB; ++i)
-#pragma unroll
-    for (int j = 0; j < TB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < C::NB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   if ((int)blockIdx.x < n_main) {
     const int ct = blockIdx.x % p.n_ct, ki = blockIdx.x / p.n_ct, parts = p.ks * ST_W, part = ki * ST_W + w;
     const int64_t c0 = (int64_t)ct * C::CW;
-    stream_steps<FP8, TB, false>(a, ring, 0, T, c0, (int)((int64_t)nk * part / parts), (int)((int64_t)nk * (part + 1) / parts), acc);
+    stream_steps<FP8, false>(a, ring, T, c0, (int)((int64_t)nk * part / parts), (int)((int64_t)nk * (part + 1) / parts), acc);
     float* out = static_cast<float*>(a.ws) + (int64_t)ki * T * a.d_out;
-#pragma unroll
-    for (int g0 = 0; g0 < C::NB; g0 += C::G)
-      sum_waves<TB, C::G>(acc, lds, g0, C::G, [&](int g, int t, int q, f32x4 s) {
-        const int64_t c = c0 + (g0 + g) * 16 + 4 * q;
-        if (t < T && c < a.d_out) *reinterpret_cast<f32x4*>(out + t * a.d_out + c) = s;
-      });
+    sum_waves<C::NB>(acc, lds, C::NB, [&](int g, int t, int q, f32x4 s) {
+      const int64_t c = c0 + g * 16 + 4 * q;
+      if (t < T && c < a.d_out) *reinterpret_cast<f32x4*>(out + t * a.d_out + c) = s;
+    });
     return;
   }
   // Adapter rows: workgroup i works for row i's agent if no earlier row has it.
@@ -243,13 +219,10 @@ __global__ void __launch_bounds__(ST_W * 64) stream_kernel(const ProjectArgs a, 
   const bool same = lane < T && a.agent[lane < T ? lane : 0] == ag;
   const uint64_t mine = __ballot(same);
   if (mine & ((1ull << i) - 1)) return;  // uniform: every wave sees the same rows
-  f32x4 (&acc4)[C::NB][TB] = acc;
-  stream_steps<FP8, TB, true>(a, ring, 0, T, (int64_t)ag * a.rank, (int)((int64_t)nk * part / parts),
-                              (int)((int64_t)nk * (part + 1) / parts), acc4);
-  float* out = static_cast<float*>(a.ws) + (int64_t)p.ks * T * a.d_out + (int64_t)ki * T * a.rank;
-  constexpr int G = 4;
-  static_assert(C::NB >= G, "blocks of rank 64");
-  sum_waves<TB, G>(acc, lds, 0, (a.rank + 15) / 16, [&](int g, int t, int q, f32x4 s) {
+  stream_steps<FP8, true>(a, ring, T, (int64_t)ag * a.rank, (int)((int64_t)nk * part / parts),
+                          (int)((int64_t)nk * (part + 1) / parts), acc);
+  float* out = static_cast<float*>(a.ws) + p.h_at + (int64_t)ki * T * a.rank;
+  sum_waves<4>(acc, lds, (a.rank + 15) / 16, [&](int g, int t, int q, f32x4 s) {
     const int j = g * 16 + 4 * q;
     if (j < a.rank && (mine >> t & 1)) *reinterpret_cast<f32x4*>(out + t * a.rank + j) = s;
   });
@@ -260,7 +233,7 @@ __global__ void __launch_bounds__(ST_W * 64) stream_kernel(const ProjectArgs a, 
 // (lanes past the last column read the row's first ones); their sums are added
 // in a fixed order.
 template <int R>
-__global__ void __launch_bounds__(256) join_kernel(const ProjectArgs a, const StreamPlan p) {
+__global__ void __launch_bounds__(256) join_kernel(const ProjectArgs a, const SlabPlan p) {
   constexpr int RW = R / 4;
   __shared__ f32x4 part[3][64];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -281,7 +254,7 @@ __global__ void __launch_bounds__(256) join_kernel(const ProjectArgs a, const St
     const uint16_t* B = a.B + ((int64_t)ag * R + w * RW) * a.d_out + c;
 #pragma unroll
     for (int j = 0; j < RW; ++j) b[j] = *reinterpret_cast<const u32x2*>(B + j * a.d_out);
-    const float* H = P + p.ks * T * a.d_out + t * R + w * RW + lane % RW;
+    const float* H = P + p.h_at + t * R + w * RW + lane % RW;
     float h = 0.f;
     for (int k = 0; k < p.ksa; ++k) h += H[k * T * R];
     const float hb = bf_lo(pack_bf16(h * xs, 0.f));
@@ -306,8 +279,8 @@ __global__ void __launch_bounds__(256) join_kernel(const ProjectArgs a, const St
 // a CU, those of the adapters (as long as W's at most) beside them.  Up to 4 rows
 // two a CU (4096 x 4096: 11.3 us against 12.3 for one row, 15.2 against 13.5 for
 // 16: the slices' sums are written and read again).
-StreamPlan stream_plan(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, bool fp8, int cus) {
-  StreamPlan p;
+SlabPlan stream_plan(int64_t T, int64_t d_in, int64_t d_out, int n_agents, bool fp8, int cus) {
+  SlabPlan p{};
   const int cw = fp8 ? 128 : 64, ad = (int)(T < n_agents ? T : n_agents);
   p.n_ct = (int)((d_out + cw - 1) / cw);
   const int64_t steps = (d_in + 31) / 32;
@@ -315,28 +288,17 @@ StreamPlan stream_plan(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int
   if (most < 1) most = 1;
   p.ks = (T <= 4 ? 2 * cus : cus) / p.n_ct;
   p.ks = p.ks < 1 ? 1 : (p.ks > most ? most : p.ks);
-  const int slots = T <= 16 ? 2 * cus : cus;
-  while (p.ks > 1 && (p.n_ct + ad) * p.ks > slots) --p.ks;
+  while (p.ks > 1 && (p.n_ct + ad) * p.ks > 2 * cus) --p.ks;
   p.ksa = ad > 0 ? p.ks : 0;
+  p.n_tt = 1;
+  p.h_at = (int64_t)p.ks * T * d_out;
   return p;
 }
-size_t stream_bytes(int64_t T, int64_t d_out, int rank, const StreamPlan& p) {
-  return ((size_t)p.ks * (size_t)T * (size_t)d_out + (size_t)p.ksa * (size_t)T * (size_t)rank) * 4;
+size_t plan_bytes(int64_t T, int rank, const SlabPlan& p) {
+  return ((size_t)p.h_at + (size_t)p.ksa * (size_t)T * (size_t)rank) * 4;
 }
 
-template <bool FP8, int TB>
-hipError_t launch_stream_tb(const ProjectArgs& a, const StreamPlan& p, hipStream_t st) {
-  const unsigned grid = (unsigned)(p.n_ct * p.ks + p.ksa * (int)a.T);
-  hipLaunchKernelGGL((stream_kernel<FP8, TB>), dim3(grid), dim3(ST_W * 64), 0, st, a, p);
-  return hipGetLastError();
-}
-
-template <bool FP8>
-hipError_t launch_stream(const ProjectArgs& a, hipStream_t st) {
-  const StreamPlan p = stream_plan(a.T, a.d_in, a.d_out, a.n_agents, a.rank, FP8, a.cus);
-  hipError_t e = a.T <= 16 ? launch_stream_tb<FP8, 1>(a, p, st)
-                           : (a.T <= 32 ? launch_stream_tb<FP8, 2>(a, p, st) : launch_stream_tb<FP8, 4>(a, p, st));
-  if (e != hipSuccess) return e;
+hipError_t launch_join(const ProjectArgs& a, const SlabPlan& p, hipStream_t st) {
   const dim3 grid((unsigned)((a.d_out + 255) / 256), (unsigned)a.T);
   switch (a.rank) {
     case 8: hipLaunchKernelGGL((join_kernel<8>), grid, dim3(256), 0, st, a, p); break;
@@ -347,54 +309,196 @@ hipError_t launch_stream(const ProjectArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <bool FP8>
+hipError_t launch_stream(const ProjectArgs& a, hipStream_t st) {
+  const SlabPlan p = stream_plan(a.T, a.d_in, a.d_out, a.n_agents, FP8, a.cus);
+  const int64_t blocks = (int64_t)p.n_ct * p.ks + (int64_t)p.ksa * a.T;
+  hipLaunchKernelGGL((stream_kernel<FP8>), dim3((unsigned)blocks), dim3(ST_W * 64), 0, st, a, p);
+  if (const hipError_t e = hipGetLastError()) return e;
+  return launch_join(a, p, st);
+}
+
 // ---------------------------------------------------------------------------
 // Many rows: X A_a of every row first, then X W in tiles with the expanded
 // adapter rows added as each tile is written.
 //
-// The adapter rows: a workgroup takes 64 rows and a slice of k, and as many of
-// their agents at a time as 64 columns hold.  Its stages (128 bytes of k) come
-// through a ring in LDS; every wave computes 16 rows x two blocks of 16 columns.
-// A's rows are short (2 r bytes, and a CU takes one request of up to 128 bytes
-// every other cycle), so A bounds it: 64 rows a workgroup share each of them.
-constexpr int SH_T = 64, SH_NB = 4;  // rows; 16-column blocks
-constexpr int SH_TURNS = 2;
+// Slabs: 64 rows x 128 bytes of weight columns x a slice of k, summed in fp32 in
+// the workspace.  They form the adapter rows X A_a for the tiles, and for calls
+// of a few hundred rows X W beside them, joined by the kernel above.  Stages (128
+// bytes of k) come through a ring in LDS with direct loads that all waves issue;
+// weight rows lie in 16-column units XOR-swizzled by row.
+//
+// Of A a workgroup takes as many of its rows' agents at a time as 64 columns
+// hold (rows with more take turns, SL_TURNS workgroups at once).  A's rows are
+// short (2 r bytes, and a CU takes one request of up to 128 bytes every other
+// cycle), so A bounds it: 64 rows share each of them.
+constexpr int SL_T = 64, SL_NB = 4;  // rows; 16-column blocks of A
+constexpr int SL_TURNS = 2;
+
 
 template <bool FP8>
-struct Shrink {
-  static constexpr int E = FP8 ? 1 : 2, KS = 128 / E;          // bytes of an element; k of a stage
-  static constexpr int XB = SH_T * 128, AB = KS * SH_NB * 32;  // bytes of X and of A
-  static constexpr int NA = AB / 8192, NI = 1 + NA;            // a wave's loads of A, and all
-  // Two workgroups a CU: one's start and end beside the other's loads (4096 rows:
-  // 11.3 us against 14.1 with one and twice the stages).
+struct Slab {
+  static constexpr int E = FP8 ? 1 : 2, KS = 128 / E, KK = KS / 32;  // bytes of an element; k and MFMA steps of a stage
+  static constexpr int CW = FP8 ? 128 : 64;                          // columns of W
+  static constexpr int XB = SL_T * 128, AB = KS * 128;               // bytes of X and of weights
+  static constexpr int NA = AB / 8192, NI = 1 + NA;                  // a wave's loads of weights, and all
+  // Two workgroups a CU: one's start and end beside the other's loads (adapter
+  // rows of 4096: 11.3 us against 14.1 with one and twice the stages).
   static constexpr int STEP = XB + AB, RING = FP8 ? 3 : 5;
   static_assert(RING * STEP <= 80 * 1024, "LDS");
 };
 
+// A slab's stages s_lo .. s_hi of this wave: load(s) issues stage s's X, then its
+// weights; use(stage) multiplies.
+template <bool FP8, typename IssueX, typename IssueW, typename Use>
+__device__ __forceinline__ void slab_stages(int s_lo, int s_hi, IssueX issue_x, IssueW issue_w, Use use) {
+  using C = Slab<FP8>;
+  __syncthreads();  // the stages of the agents before are read
+  for (int i = 0; i < C::RING - 1; ++i) issue_x(s_lo + i, i);
+  for (int i = 0; i < C::RING - 1; ++i) issue_w(s_lo + i, i);
+  int slot = 0, last = C::RING - 1;
+  for (int s = s_lo; s < s_hi; ++s) {
+    // After stage s came the weights of the RING - 2 first stages, or all of as many.
+    if (s < s_lo + C::RING - 1) wait_loads<(C::RING - 2) * C::NA>();
+    else wait_loads<(C::RING - 2) * C::NI>();
+    wait_lds();
+    __builtin_amdgcn_s_barrier();  // stage s has landed, stage s - 1 is read
+    asm volatile("" ::: "memory");
+    issue_x(s + C::RING - 1, last);
+    issue_w(s + C::RING - 1, last);
+    use(slot);
+    last = slot;
+    slot = slot + 1 == C::RING ? 0 : slot + 1;
+  }
+  wait_loads<0>();
+}
+
 template <bool FP8>
-__global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ksa) {
-  using C = Shrink<FP8>;  // workgroup (ki + ksa * rows, turn)
+__global__ void __launch_bounds__(512, 4) slab_kernel(const ProjectArgs a, const SlabPlan p) {
+  using C = Slab<FP8>;
   constexpr int E = C::E;
   __shared__ __attribute__((aligned(1024))) char ring[C::RING * C::STEP];
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, c16 = lane & 15;
-  const int ki = (int)(blockIdx.x % (unsigned)ksa), R = a.rank, rp = R < 16 ? 16 : R;
-  const int64_t t0 = (int64_t)(blockIdx.x / (unsigned)ksa) * SH_T;
-  const int toks = (int)(a.T - t0 < SH_T ? a.T - t0 : (int64_t)SH_T), d_in = (int)a.d_in;
+  // Workgroup L runs on XCD L % 8: each takes an eighth of the slabs of W, row
+  // tiles fastest (they share columns), then those of the adapters follow.
+  const int n_main = p.n_ct * p.n_tt * p.ks, per = (n_main + 7) / 8, L = (int)blockIdx.x;
+  const bool ad = L >= 8 * per;
+  const int m = ad ? L - 8 * per : L % 8 * per + L / 8;
+  if (!ad && m >= n_main) return;  // uniform over the workgroup
+  const int ks = ad ? p.ksa : p.ks;
+  const int tt = __builtin_amdgcn_readfirstlane(ad ? m / SL_TURNS / p.ksa : m % p.n_tt), ct = ad ? 0 : m / p.n_tt % p.n_ct;
+  const int ki = __builtin_amdgcn_readfirstlane(ad ? m / SL_TURNS % p.ksa : m / p.n_tt / p.n_ct);
+  const int64_t t0 = (int64_t)tt * SL_T;
+  const int toks = (int)(a.T - t0 < SL_T ? a.T - t0 : (int64_t)SL_T), d_in = (int)a.d_in;
   const int nk = (d_in + C::KS - 1) / C::KS;
-  const int s_lo = (int)((int64_t)nk * ki / ksa), s_hi = (int)((int64_t)nk * (ki + 1) / ksa);
-  const int ag = lane < toks ? a.agent[t0 + lane] : -1;
-  uint64_t todo = __ballot(ag >= 0 && ag < a.n_agents);  // the same in every wave
-  float* H = static_cast<float*>(a.ws) + ((int64_t)ki * a.T + t0) * R;
-  const int32_t lda = (int32_t)((int64_t)a.n_agents * R * 2), ldx = (int32_t)(a.ld_x * E);
-  const i32x4 ra = buffer_rsrc(a.A, d_in * lda);
+  const int s_lo = (int)((int64_t)nk * ki / ks), s_hi = (int)((int64_t)nk * (ki + 1) / ks);
+  const int32_t ldx = (int32_t)(a.ld_x * E);
   const i32x4 rx = buffer_rsrc(static_cast<const char*>(a.X) + t0 * ldx, (toks - 1) * ldx + d_in * E);
   // X: rows 8 wv .. of this wave, 16-byte chunks XOR-swizzled by row.
   const int xr = 8 * wv + lane / 8, kx = ((lane % 8) ^ ((xr >> 1) & 7)) * 16 / E;
   const int32_t ox = xr < toks ? xr * ldx + kx * E : INT32_MIN;
+  auto issue_x = [&](int s, int slot) {
+    const int k0 = s * C::KS, left = s < s_hi ? d_in - k0 : 0;
+    lds_dma16(rx, ring + slot * C::STEP + wv * 1024, kx < left && ox != INT32_MIN ? ox + k0 * E : INT32_MIN, 0);
+  };
+  // Weights: rows 8 (8 j + wv) .. of 128 bytes, from byte offsets ow of rows kw.
+  int32_t kw[C::NA], ow[C::NA];
+  auto issue_w = [&](i32x4 r, int32_t ld, int s, int slot) {
+    const int k0 = s * C::KS, left = s < s_hi ? d_in - k0 : 0;
+#pragma unroll
+    for (int j = 0; j < C::NA; ++j)
+      lds_dma16(r, ring + slot * C::STEP + C::XB + (8 * j + wv) * 1024,
+                kw[j] < left && ow[j] != INT32_MIN ? (int32_t)((uint32_t)ow[j] + (uint32_t)k0 * (uint32_t)ld) : INT32_MIN, 0);
+  };
+  // This wave's rows 16 tb ..; of bf16 weights blocks cb and cb + 2, of e4m3 four from 4 cb.
+  const int tb = wv & 3, cb = wv >> 2, row = 16 * tb + c16, xs = (row >> 1) & 7;
+  const int64_t t = t0 + row;
+  // The MFMAs of a stage with bf16 weights: all fragments first, one wait for them.
+  auto use16 = [&](int slot, f32x4 (&acc)[2]) {
+    const char* st = ring + slot * C::STEP;
+    bf16x8 x[C::KK], w[C::KK][2];
+#pragma unroll
+    for (int kk = 0; kk < C::KK; ++kk) {
+      const char* xp = st + row * 128;
+      if constexpr (FP8)
+        x[kk] = as_bf16x8(bf16_of_e4m3(*reinterpret_cast<const u32x2*>(xp + ((2 * kk + q / 2) ^ xs) * 16 + q % 2 * 8)));
+      else
+        x[kk] = as_bf16x8(*reinterpret_cast<const u32x4*>(xp + ((4 * kk + q) ^ xs) * 16));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = 8 * q + c16 / 4;  // row r + 4 and those 32 further swizzle alike
+        const char* wp = st + C::XB + (32 * kk + r) * 128 + ((cb + 2 * i) ^ swz<false>(r)) * 32 + c16 % 4 * 8;
+        const u32x2 lo = lds_read_tr16(wp), hi = lds_read_tr16(wp + 512);
+        w[kk][i] = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
+      }
+    }
+#pragma unroll
+    for (int kk = 0; kk < C::KK; ++kk)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) acc[i] = mfma16x16x32(w[kk][i], x[kk], acc[i]);
+  };
+
+  if (!ad) {
+    const int64_t c0 = (int64_t)ct * C::CW;
+    const int32_t ldw = (int32_t)(a.d_out * E);
+    const i32x4 rw = buffer_rsrc(a.W, d_in * ldw);
+#pragma unroll
+    for (int j = 0; j < C::NA; ++j) {
+      const int k = (8 * j + wv) * 8 + lane / 8, c = FP8 ? ((lane % 8) ^ swz<true>(k)) * 16 : ((lane % 8 / 2) ^ swz<false>(k)) * 16 + lane % 2 * 8;
+      kw[j] = k;
+      ow[j] = c0 + c < a.d_out ? k * ldw + (int32_t)(c0 + c) * E : INT32_MIN;
+    }
+    auto issue = [&](int s, int slot) { issue_w(rw, ldw, s, slot); };
+    float* out = static_cast<float*>(a.ws) + ((int64_t)ki * a.T + t) * a.d_out + c0;
+    if constexpr (!FP8) {
+      f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      slab_stages<FP8>(s_lo, s_hi, issue_x, issue, [&](int slot) { use16(slot, acc); });
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int c = (cb + 2 * i) * 16 + 4 * q;
+        if (row < toks && c0 + c < a.d_out) *reinterpret_cast<f32x4*>(out + c) = acc[i];
+      }
+    } else {
+      f32x4 acc[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      slab_stages<FP8>(s_lo, s_hi, issue_x, issue, [&](int slot) {
+        const char* st = ring + slot * C::STEP;
+        long x[C::KK], w[C::KK][4];
+#pragma unroll
+        for (int kk = 0; kk < C::KK; ++kk) {
+          x[kk] = *reinterpret_cast<const long*>(st + row * 128 + ((2 * kk + q / 2) ^ xs) * 16 + q % 2 * 8);
+          const int r = 32 * kk + 8 * q + c16 / 2;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            w[kk][i] = __builtin_bit_cast(long, lds_read_tr8(st + C::XB + r * 128 + ((4 * cb + i) ^ swz<true>(r)) * 16 + c16 % 2 * 8));
+        }
+#pragma unroll
+        for (int kk = 0; kk < C::KK; ++kk)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(w[kk][i], x[kk], acc[i], 0, 0, 0);
+      });
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = (4 * cb + i) * 16 + 4 * q;
+        if (row < toks && c0 + c < a.d_out) *reinterpret_cast<f32x4*>(out + c) = acc[i];
+      }
+    }
+    return;
+  }
+
+  // ---- adapter rows ------------------------------------------------------------
+  const int R = a.rank, rp = R < 16 ? 16 : R;
+  const int ag = lane < toks ? a.agent[t0 + lane] : -1, own = row < toks ? a.agent[t] : -1;
+  uint64_t todo = __ballot(ag >= 0 && ag < a.n_agents);  // the same in every wave
+  float* H = static_cast<float*>(a.ws) + p.h_at + ((int64_t)ki * a.T + t0) * R;
+  const int32_t lda = (int32_t)((int64_t)a.n_agents * R * 2);
+  const i32x4 ra = buffer_rsrc(a.A, d_in * lda);
   for (int turn = 0; todo != 0; ++turn) {
     // The agents of blocks 0 .. 3 (-1: none).
-    int id[SH_NB];
+    int id[SL_NB];
 #pragma unroll
-    for (int b = 0; b < SH_NB; ++b) {
+    for (int b = 0; b < SL_NB; ++b) {
       if (b * 16 % rp != 0) {  // another block of the same agent
         id[b] = b > 0 ? id[b - 1] : -1;
         continue;
@@ -402,73 +506,18 @@ __global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ks
       id[b] = todo != 0 ? __builtin_amdgcn_readlane(ag, __builtin_ctzll(todo)) : -1;
       if (todo != 0) todo &= ~__ballot(ag == id[b]);
     }
-    // Rows with more agents than that take turns, SH_TURNS workgroups at once.
-    if (turn % SH_TURNS != (int)blockIdx.y) continue;  // uniform
-    // A: rows of 128 bytes (four blocks of 16 columns), blocks XOR-swizzled by
-    // row so that the rows of one read hit different banks.
-    int32_t ka[C::NA], oa[C::NA];
+    if (turn % SL_TURNS != m % SL_TURNS) continue;  // uniform
 #pragma unroll
     for (int j = 0; j < C::NA; ++j) {
       const int k = (8 * j + wv) * 8 + lane / 8, blk = (lane % 8 / 2) ^ swz<false>(k), c = blk * 16 % rp + lane % 2 * 8;
-      int own = id[0];
+      int mine = id[0];
 #pragma unroll
-      for (int i = 1; i < SH_NB; ++i) own = blk == i ? id[i] : own;
-      ka[j] = k;
-      oa[j] = own >= 0 && c < R ? k * lda + (own * R + c) * 2 : INT32_MIN;
+      for (int i = 1; i < SL_NB; ++i) mine = blk == i ? id[i] : mine;
+      kw[j] = k;
+      ow[j] = mine >= 0 && c < R ? k * lda + (mine * R + c) * 2 : INT32_MIN;
     }
-    auto issue_x = [&](int s) {
-      const int k0 = s * C::KS, left = s < s_hi ? d_in - k0 : 0;
-      lds_dma16(rx, ring + (s - s_lo) % C::RING * C::STEP + wv * 1024, kx < left && ox != INT32_MIN ? ox + k0 * E : INT32_MIN, 0);
-    };
-    auto issue_a = [&](int s) {
-      const int k0 = s * C::KS, left = s < s_hi ? d_in - k0 : 0;
-#pragma unroll
-      for (int j = 0; j < C::NA; ++j)
-        lds_dma16(ra, ring + (s - s_lo) % C::RING * C::STEP + C::XB + (8 * j + wv) * 1024,
-                  ka[j] < left && oa[j] != INT32_MIN ? (int32_t)((uint32_t)oa[j] + (uint32_t)k0 * (uint32_t)lda) : INT32_MIN, 0);
-    };
-    // This wave's rows 16 tb .. and blocks cb and cb + 2.
-    const int tb = wv & 3, cb = wv >> 2, row = 16 * tb + c16, xs = (row >> 1) & 7;
     f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    __syncthreads();  // the stages of the agents before are read
-    for (int i = 0; i < C::RING - 1; ++i) issue_x(s_lo + i);
-    for (int i = 0; i < C::RING - 1; ++i) issue_a(s_lo + i);
-    for (int s = s_lo; s < s_hi; ++s) {
-      // After stage s came the A of the RING - 2 first stages, or both of as many.
-      if (s < s_lo + C::RING - 1) wait_loads<(C::RING - 2) * C::NA>();
-      else wait_loads<(C::RING - 2) * C::NI>();
-      wait_lds();
-      __builtin_amdgcn_s_barrier();  // stage s has landed, stage s - 1 is read
-      asm volatile("" ::: "memory");
-      issue_x(s + C::RING - 1);
-      issue_a(s + C::RING - 1);
-      const char* st = ring + (s - s_lo) % C::RING * C::STEP;
-      // All of the stage's fragments, then its MFMAs (blocks without an agent are
-      // zeros): one wait a stage, not one a product.
-      constexpr int KK = C::KS / 32;
-      bf16x8 x[KK], w[KK][2];
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        const char* xp = st + row * 128;
-        if constexpr (FP8)
-          x[kk] = as_bf16x8(bf16_of_e4m3(*reinterpret_cast<const u32x2*>(xp + ((2 * kk + q / 2) ^ xs) * 16 + q % 2 * 8)));
-        else
-          x[kk] = as_bf16x8(*reinterpret_cast<const u32x4*>(xp + ((4 * kk + q) ^ xs) * 16));
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int r = 8 * q + c16 / 4;  // row r + 4 and those 32 further swizzle alike
-          const char* p = st + C::XB + (32 * kk + r) * 128 + ((cb + 2 * i) ^ swz<false>(r)) * 32 + c16 % 4 * 8;
-          const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 512);
-          w[kk][i] = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
-        }
-      }
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) acc[i] = mfma16x16x32(w[kk][i], x[kk], acc[i]);
-    }
-    wait_loads<0>();
-    const int own = row < toks ? a.agent[t0 + row] : -1;
+    slab_stages<FP8>(s_lo, s_hi, issue_x, [&](int s, int slot) { issue_w(ra, lda, s, slot); }, [&](int slot) { use16(slot, acc); });
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int j = (cb + 2 * i) * 16 % rp + 4 * q;
@@ -477,10 +526,17 @@ __global__ void __launch_bounds__(512) shrink_kernel(const ProjectArgs a, int ks
   }
 }
 
+template <bool FP8>
+hipError_t launch_slabs(const ProjectArgs& a, const SlabPlan& p, hipStream_t st) {
+  const int64_t n_main = (int64_t)p.n_ct * p.n_tt * p.ks, n_ad = (a.T + SL_T - 1) / SL_T * p.ksa * SL_TURNS;
+  hipLaunchKernelGGL((slab_kernel<FP8>), dim3((unsigned)((n_main + 7) / 8 * 8 + n_ad)), dim3(512), 0, st, a, p);
+  return hipGetLastError();
+}
+
 // k slices of the adapter rows: enough workgroups for the CUs, two stages each at
 // least; no more than 256 sums a row, which every tile of the row adds.
 int shrink_slices(int64_t T, int64_t d_in, int rank, int cus) {
-  const int64_t rows = (T + SH_T - 1) / SH_T, most = d_in / 256, sums = 256 / rank;
+  const int64_t rows = (T + SL_T - 1) / SL_T, most = d_in / 256, sums = 256 / rank;
   int64_t k = cus / rows;
   k = k > most ? most : k;
   k = k > sums ? sums : k;
@@ -1201,13 +1257,30 @@ hipError_t launch_mid(const ProjectArgs& a, int ksa, hipStream_t st) {
   return hipGetLastError();
 }
 
+// k slices of the slabs, the same of W and of the adapters: a slab a CU, a stage
+// each at least.  (Two a CU: 4096 x 4096 no faster, 2048 x 2048 in e4m3 14.7 us
+// against 12.6 for 48 rows: more sums to write and read.)
+SlabPlan slab_plan(int64_t T, int64_t d_in, int64_t d_out, int n_agents, bool fp8, int cus) {
+  SlabPlan p{};
+  const int cw = fp8 ? 128 : 64;
+  p.n_ct = (int)((d_out + cw - 1) / cw);
+  p.n_tt = (int)((T + SL_T - 1) / SL_T);
+  const int64_t most = (d_in + 127) / 128;
+  int64_t k = cus / ((int64_t)(p.n_ct + 1) * p.n_tt);  // (one for the adapters)
+  k = k > most ? most : k;
+  p.ks = (int)(k < 1 ? 1 : (k > 8 ? 8 : k));
+  p.ksa = n_agents > 0 ? p.ks : 0;
+  p.h_at = (int64_t)p.ks * T * d_out;
+  return p;
+}
+
 // The tile shape that takes the least time.  A CU holds one tile at a time, so a
 // launch takes as many rounds as its tiles fill the CUs; a round takes a fixed
 // time and one that goes with d_in (microseconds, the latter at 4096), less in a
 // round that leaves CUs idle (down to about 0.6 of it: the clock rises), and
 // more where adapter rows are added.  Measured with 256 tiles at d_in 1024 and
 // 4096, bf16 and e4m3.
-int tile_form(const ProjectArgs& a, bool fp8) {
+int tile_form(int64_t T, int64_t d_in, int64_t d_out, int n_agents, bool fp8, int cus, double* us) {
   struct Form {
     int toks, cols;
     double fixed[2], per[2], lr;
@@ -1221,27 +1294,58 @@ int tile_form(const ProjectArgs& a, bool fp8) {
   double least = 1e300;
   for (int i = 0; i < 6; ++i) {
     const Form& f = forms[i];
-    const int64_t tiles = ((a.T + f.toks - 1) / f.toks) * ((a.d_out + f.cols - 1) / f.cols), rounds = tiles / a.cus,
-                  rest = tiles % a.cus;
-    const double fixed = f.fixed[fp8] + (a.n_agents > 0 ? f.lr : 0.0), per = f.per[fp8] * (double)a.d_in / 4096.0;
-    const double t = (double)rounds * (fixed + per) + (rest > 0 ? fixed + per * (0.6 + 0.4 * (double)rest / a.cus) : 0.0);
+    const int64_t tiles = ((T + f.toks - 1) / f.toks) * ((d_out + f.cols - 1) / f.cols), rounds = tiles / cus,
+                  rest = tiles % cus;
+    const double fixed = f.fixed[fp8] + (n_agents > 0 ? f.lr : 0.0), per = f.per[fp8] * (double)d_in / 4096.0;
+    const double t = (double)rounds * (fixed + per) + (rest > 0 ? fixed + per * (0.6 + 0.4 * (double)rest / cus) : 0.0);
     if (t < least) {
       least = t;
       best = i;
     }
   }
+  *us = least;
   return best;
+}
+
+// Slabs or tiles.  Slabs fill the CUs where tiles would leave most idle, and form
+// the adapter rows beside the others, but read X and W more often and their sums
+// once more; they run at the rate of the L2s (11 TB/s) on their stages, the sums
+// and, for each row, its agent's B.  Measured for 96 to 512 rows of 1024 x 1024
+// to 14336 x 4096 and 4096 x 14336, in bf16 with rank 16 and e4m3 with rank 64:
+// 4096 x 4096, 96 rows 19.6 us as slabs against 29.2, 512 rows 57.8 against 34.4;
+// 14336 x 4096 in e4m3, 160 rows 35.6 against 61.9.  Up to 64 rows always: less
+// than a tile's.  The rule takes adapters of rank 32 for granted, so that a row
+// without one has the same bits whether others have theirs or no call does.
+constexpr int SL_MOST = 1024;  // bounds the workspace
+
+bool slabs_pay(int64_t T, int64_t d_in, int64_t d_out, bool fp8, int cus) {
+  if (T <= SL_T || T > SL_MOST) return T <= SL_T;
+  const SlabPlan p = slab_plan(T, d_in, d_out, 1, fp8, cus);
+  const int ks = fp8 ? 128 : 64;
+  const double stages = (double)p.n_ct * p.n_tt * (double)((d_in + ks - 1) / ks), out = (double)T * (double)d_out;
+  const double bytes = stages * (fp8 ? 24576.0 : 16384.0) + out * (8.0 * p.ks + 2.0 * 32);
+  double us;
+  tile_form(T, d_in, d_out, 1, fp8, cus, &us);
+  return 8.0 + bytes / 11e6 < us + 3.0 + 8.0 * (double)d_in / 4096.0;  // (the launch for the adapter rows)
 }
 
 template <bool FP8>
 hipError_t launch(const ProjectArgs& a, hipStream_t st) {
   if (a.T <= ST_T) return launch_stream<FP8>(a, st);
+  if (slabs_pay(a.T, a.d_in, a.d_out, FP8, a.cus)) {
+    const SlabPlan p = slab_plan(a.T, a.d_in, a.d_out, a.n_agents, FP8, a.cus);
+    if (const hipError_t e = launch_slabs<FP8>(a, p, st)) return e;
+    return launch_join(a, p, st);
+  }
   const int ksa = shrink_slices(a.T, a.d_in, a.rank, a.cus);
   if (a.n_agents > 0) {
-    hipLaunchKernelGGL((shrink_kernel<FP8>), dim3((unsigned)((a.T + SH_T - 1) / SH_T * ksa), SH_TURNS), dim3(512), 0, st, a, ksa);
-    if (const hipError_t e = hipGetLastError()) return e;
+    SlabPlan p{};
+    p.n_tt = 1;
+    p.ksa = ksa;
+    if (const hipError_t e = launch_slabs<FP8>(a, p, st)) return e;
   }
-  switch (tile_form(a, FP8)) {
+  double us;
+  switch (tile_form(a.T, a.d_in, a.d_out, a.n_agents, FP8, a.cus, &us)) {
     case 0: return launch_mid<FP8, 2>(a, ksa, st);
     case 1: return launch_mid<FP8, 4>(a, ksa, st);
     case 2: return launch_tiles<FP8, 2, 2>(a, ksa, st);
@@ -1255,12 +1359,16 @@ hipError_t launch(const ProjectArgs& a, hipStream_t st) {
 
 size_t adapted_projection_bytes(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, int cus) {
   if (n_agents == 0) rank = 8;
-  if (T <= ST_T) {
-    const size_t a = stream_bytes(T, d_out, rank, stream_plan(T, d_in, d_out, n_agents, rank, false, cus));
-    const size_t b = stream_bytes(T, d_out, rank, stream_plan(T, d_in, d_out, n_agents, rank, true, cus));
-    return a > b ? a : b;
+  size_t most = 0;
+  for (const bool fp8 : {false, true}) {
+    size_t b = n_agents > 0 ? (size_t)shrink_slices(T, d_in, rank, cus) * (size_t)T * (size_t)rank * 4 : 0;
+    if (T <= ST_T)
+      b = plan_bytes(T, rank, stream_plan(T, d_in, d_out, n_agents, fp8, cus));
+    else if (slabs_pay(T, d_in, d_out, fp8, cus))
+      b = plan_bytes(T, rank, slab_plan(T, d_in, d_out, n_agents, fp8, cus));
+    most = b > most ? b : most;
   }
-  return n_agents > 0 ? (size_t)shrink_slices(T, d_in, rank, cus) * (size_t)T * (size_t)rank * 4 : 0;
+  return most;
 }
 
 hipError_t launch_adapted_projection(const ProjectArgs& a, hipStream_t st) {

@@ -149,6 +149,25 @@ def test_projection_tile_shapes(T, k, n, N, r, order, fp8):
     check_project(call(prc, c), *ref_of(c))
 
 
+# A few hundred rows as 64-row slabs: one and several k slices, ends inside a slab, a stage and 16 columns; more
+# agents among 64 rows than are taken at once; 128 x 64 tiles where there are too many slabs.
+SHAPES_SLABS = [(17, 136, 72), (47, 4112, 272), (64, 64, 4096), (66, 1032, 3080), (191, 2056, 1032), (257, 5128, 520),
+                (1000, 1096, 200), (1024, 72, 1048), (300, 3592, 4096), (90, 520, 40000)]
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("N,r,order", [(200, 64, "mixed"), (9, 32, "some"), (40, 16, "mixed"), (30, 8, "mixed"), (0, 0, "none")])
+@pytest.mark.parametrize("T,k,n", SHAPES_SLABS)
+def test_projection_slab_shapes(T, k, n, N, r, order, fp8):
+    if fp8:
+        k, n = (k + 15) // 16 * 16, (n + 15) // 16 * 16
+    print(f"project {T} {k} {n} {N} r{r} {order} fp8={fp8}", flush=True)
+    c = project_case(T + k + n + r, T, k, n, N, r, order, fp8)
+    got = call(prc, c)
+    check_project(got, *ref_of(c))
+    assert torch.equal(got, call(prc, c))
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("T,k,n", SHAPES_TILES[1:6])
 def test_bad_adapters_stay_in_their_rows_of_wide_tiles(T, k, n, fp8):
