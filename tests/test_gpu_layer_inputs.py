@@ -34,6 +34,14 @@ def test_norm(T, d, residual):
     assert residual or out is None
 
 
+@pytest.mark.parametrize("residual", [True, False])
+@pytest.mark.parametrize("T", [3, 1031])
+@pytest.mark.parametrize("d", [504, 512, 520, 1024, 1032, 2048, 2064, 4096, 4112, 16384, 16400, 32768])
+def test_norm_widths(T, d, residual):
+    """Ends of what a row's threads hold, whole and ragged, with a workgroup's last rows missing."""
+    test_norm(T, d, residual)
+
+
 def test_norm_of_strided_rows_leaves_the_gaps():
     T, d = 37, 264
     x, w, res = norm_case(T, d, True)
