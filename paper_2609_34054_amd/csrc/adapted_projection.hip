@@ -187,6 +187,7 @@ __device__ __forceinline__ void sum_waves(f32x4 (&acc)[NB], char* lds, int n, Pu
 struct SlabPlan {
   int n_ct, n_tt, ks;  // column tiles of W (0: the adapter rows alone), row tiles, k slices
   int ksa;             // k slices of the adapter rows (0: none)
+  int turns;           // slabs that share the agents of a row tile and slice
   int64_t h_at;        // fp32 words before their sums
 };
 
@@ -329,11 +330,10 @@ hipError_t launch_stream(const ProjectArgs& a, hipStream_t st) {
 // weight rows lie in 16-column units XOR-swizzled by row.
 //
 // Of A a workgroup takes as many of its rows' agents at a time as 64 columns
-// hold (rows with more take turns, SL_TURNS workgroups at once).  A's rows are
+// hold; rows with more take turns, several workgroups at once.  A's rows are
 // short (2 r bytes, and a CU takes one request of up to 128 bytes every other
 // cycle), so A bounds it: 64 rows share each of them.
 constexpr int SL_T = 64, SL_NB = 4;  // rows; 16-column blocks of A
-constexpr int SL_TURNS = 2;
 
 
 template <bool FP8>
@@ -386,8 +386,8 @@ __global__ void __launch_bounds__(512, 4) slab_kernel(const ProjectArgs a, const
   const int m = ad ? L - 8 * per : L % 8 * per + L / 8;
   if (!ad && m >= n_main) return;  // uniform over the workgroup
   const int ks = ad ? p.ksa : p.ks;
-  const int tt = __builtin_amdgcn_readfirstlane(ad ? m / SL_TURNS / p.ksa : m % p.n_tt), ct = ad ? 0 : m / p.n_tt % p.n_ct;
-  const int ki = __builtin_amdgcn_readfirstlane(ad ? m / SL_TURNS % p.ksa : m / p.n_tt / p.n_ct);
+  const int tt = __builtin_amdgcn_readfirstlane(ad ? m / p.turns / p.ksa : m % p.n_tt), ct = ad ? 0 : m / p.n_tt % p.n_ct;
+  const int ki = __builtin_amdgcn_readfirstlane(ad ? m / p.turns % p.ksa : m / p.n_tt / p.n_ct);
   const int64_t t0 = (int64_t)tt * SL_T;
   const int toks = (int)(a.T - t0 < SL_T ? a.T - t0 : (int64_t)SL_T), d_in = (int)a.d_in;
   const int nk = (d_in + C::KS - 1) / C::KS;
@@ -506,7 +506,7 @@ __global__ void __launch_bounds__(512, 4) slab_kernel(const ProjectArgs a, const
       id[b] = todo != 0 ? __builtin_amdgcn_readlane(ag, __builtin_ctzll(todo)) : -1;
       if (todo != 0) todo &= ~__ballot(ag == id[b]);
     }
-    if (turn % SL_TURNS != m % SL_TURNS) continue;  // uniform
+    if (turn % p.turns != m % p.turns) continue;  // uniform
 #pragma unroll
     for (int j = 0; j < C::NA; ++j) {
       const int k = (8 * j + wv) * 8 + lane / 8, blk = (lane % 8 / 2) ^ swz<false>(k), c = blk * 16 % rp + lane % 2 * 8;
@@ -528,19 +528,31 @@ __global__ void __launch_bounds__(512, 4) slab_kernel(const ProjectArgs a, const
 
 template <bool FP8>
 hipError_t launch_slabs(const ProjectArgs& a, const SlabPlan& p, hipStream_t st) {
-  const int64_t n_main = (int64_t)p.n_ct * p.n_tt * p.ks, n_ad = (a.T + SL_T - 1) / SL_T * p.ksa * SL_TURNS;
+  const int64_t n_main = (int64_t)p.n_ct * p.n_tt * p.ks, n_ad = (a.T + SL_T - 1) / SL_T * p.ksa * p.turns;
   hipLaunchKernelGGL((slab_kernel<FP8>), dim3((unsigned)((n_main + 7) / 8 * 8 + n_ad)), dim3(512), 0, st, a, p);
   return hipGetLastError();
 }
 
-// k slices of the adapter rows: enough workgroups for the CUs, two stages each at
-// least; no more than 256 sums a row, which every tile of the row adds.
+// k slices of the adapter rows alone: enough workgroups for the CUs, two stages
+// each at least; no more than 256 sums a row, which every tile of the row adds.
 int shrink_slices(int64_t T, int64_t d_in, int rank, int cus) {
   const int64_t rows = (T + SL_T - 1) / SL_T, most = d_in / 256, sums = 256 / rank;
   int64_t k = cus / rows;
   k = k > most ? most : k;
   k = k > sums ? sums : k;
   return (int)(k < 1 ? 1 : (k > 8 ? 8 : k));
+}
+
+// Turns: as many as 64 rows' agents may need and as `room` workgroups, which run
+// at once anyhow, hold for `each` row tile and slice.  (24 rows of 4096 x 4096 in
+// e4m3 of as many agents of rank 64: two turns 19.9 us, eight 15.8; 256 rows 64.6
+// and 27.7.  Workgroups without a turn that do not fit cost: 4096 rows with eight
+// 157 us against 127.)
+int slab_turns(int n_agents, int rank, int64_t room, int64_t each) {
+  const int64_t own = SL_NB * 16 / (rank < 16 ? 16 : rank), need = ((n_agents < SL_T ? n_agents : SL_T) + own - 1) / own;
+  int64_t n = room / each;
+  n = n > need ? need : n;
+  return (int)(n < 1 ? 1 : (n > 8 ? 8 : n));
 }
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -1257,19 +1269,32 @@ hipError_t launch_mid(const ProjectArgs& a, int ksa, hipStream_t st) {
   return hipGetLastError();
 }
 
-// k slices of the slabs, the same of W and of the adapters: a slab a CU, a stage
-// each at least.  (Two a CU: 4096 x 4096 no faster, 2048 x 2048 in e4m3 14.7 us
-// against 12.6 for 48 rows: more sums to write and read.)
-SlabPlan slab_plan(int64_t T, int64_t d_in, int64_t d_out, int n_agents, bool fp8, int cus) {
+// The time of slabs in `ks` slices, in microseconds: a stage takes 0.29 while a CU
+// has one workgroup and 0.56 with two (96 rows of 4096 x 4096 in bf16: one slice,
+// on half the CUs, 27.3 us, three 19.1; four, which do not run at once, 24.2), the
+// stages together no less than W takes at the rate of a copy (24 rows of 4096 x
+// 14336: one slice 30.5 us, two 36.7); sums are written and read at 3.5 TB/s (256
+// rows of 1024 x 1024: three slices 10.8 us, seven 13.9), each row's B at 11.
+double slab_time(int64_t T, int64_t d_in, int64_t d_out, int rank, bool fp8, int cus, int ks) {
+  const int64_t cw = fp8 ? 128 : 64, n = ((d_out + cw - 1) / cw + 1) * ((T + SL_T - 1) / SL_T) * ks, nk = (d_in + cw - 1) / cw;
+  const int64_t rounds = (n + 2 * cus - 1) / (2 * cus);
+  const double fill = n < cus ? 1.0 : (rounds > 1 ? 2.0 : (double)n / cus), out = (double)T * (double)d_out;
+  const double stages = (double)(rounds * ((nk + ks - 1) / ks)) * (0.29 + 0.27 * (fill - 1.0));
+  const double once = (double)d_in * (double)d_out * (fp8 ? 1.0 : 2.0) / 5e6;
+  return 7.5 + (stages > once ? stages : once) + out * 8.0 * ks / 3.5e6 + out * 2.0 * rank / 11e6;
+}
+
+// The same k slices of W and of the adapters.
+SlabPlan slab_plan(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, bool fp8, int cus) {
   SlabPlan p{};
   const int cw = fp8 ? 128 : 64;
   p.n_ct = (int)((d_out + cw - 1) / cw);
   p.n_tt = (int)((T + SL_T - 1) / SL_T);
-  const int64_t most = (d_in + 127) / 128;
-  int64_t k = cus / ((int64_t)(p.n_ct + 1) * p.n_tt);  // (one for the adapters)
-  k = k > most ? most : k;
-  p.ks = (int)(k < 1 ? 1 : (k > 8 ? 8 : k));
+  p.ks = 1;
+  for (int k = 2; k <= 8 && k <= (d_in + 127) / 128; ++k)
+    if (slab_time(T, d_in, d_out, rank, fp8, cus, k) < slab_time(T, d_in, d_out, rank, fp8, cus, p.ks)) p.ks = k;
   p.ksa = n_agents > 0 ? p.ks : 0;
+  p.turns = n_agents > 0 ? slab_turns(n_agents, rank, 2 * cus - (int64_t)p.n_ct * p.n_tt * p.ks, (int64_t)p.n_tt * p.ks) : 1;
   p.h_at = (int64_t)p.ks * T * d_out;
   return p;
 }
@@ -1309,31 +1334,27 @@ int tile_form(int64_t T, int64_t d_in, int64_t d_out, int n_agents, bool fp8, in
 
 // Slabs or tiles.  Slabs fill the CUs where tiles would leave most idle, and form
 // the adapter rows beside the others, but read X and W more often and their sums
-// once more; they run at the rate of the L2s (11 TB/s) on their stages, the sums
-// and, for each row, its agent's B.  Measured for 96 to 512 rows of 1024 x 1024
-// to 14336 x 4096 and 4096 x 14336, in bf16 with rank 16 and e4m3 with rank 64:
-// 4096 x 4096, 96 rows 19.6 us as slabs against 29.2, 512 rows 57.8 against 34.4;
-// 14336 x 4096 in e4m3, 160 rows 35.6 against 61.9.  Up to 64 rows always: less
-// than a tile's.  The rule takes adapters of rank 32 for granted, so that a row
-// without one has the same bits whether others have theirs or no call does.
+// once more.  Measured for 96 to 512 rows of 1024 x 1024 to 14336 x 4096 and 4096
+// x 14336, in bf16 with rank 16 and e4m3 with rank 64: 4096 x 4096, 96 rows 19.1
+// us as slabs against 29.2, 512 rows 57.8 against 34.4; 14336 x 4096 in e4m3, 160
+// rows 35.6 against 61.9.  Up to 64 rows always: less than a tile's.  Without adapters
+// (n_agents 0) it goes as with some of rank 16.
 constexpr int SL_MOST = 1024;  // bounds the workspace
 
-bool slabs_pay(int64_t T, int64_t d_in, int64_t d_out, bool fp8, int cus) {
+bool slabs_pay(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, bool fp8, int cus) {
   if (T <= SL_T || T > SL_MOST) return T <= SL_T;
-  const SlabPlan p = slab_plan(T, d_in, d_out, 1, fp8, cus);
-  const int ks = fp8 ? 128 : 64;
-  const double stages = (double)p.n_ct * p.n_tt * (double)((d_in + ks - 1) / ks), out = (double)T * (double)d_out;
-  const double bytes = stages * (fp8 ? 24576.0 : 16384.0) + out * (8.0 * p.ks + 2.0 * 32);
+  if (n_agents == 0) rank = 16;
+  const SlabPlan p = slab_plan(T, d_in, d_out, n_agents, rank, fp8, cus);
   double us;
   tile_form(T, d_in, d_out, 1, fp8, cus, &us);
-  return 8.0 + bytes / 11e6 < us + 3.0 + 8.0 * (double)d_in / 4096.0;  // (the launch for the adapter rows)
+  return slab_time(T, d_in, d_out, rank, fp8, cus, p.ks) < us + 3.0 + 8.0 * (double)d_in / 4096.0;  // (the adapter rows' launch)
 }
 
 template <bool FP8>
 hipError_t launch(const ProjectArgs& a, hipStream_t st) {
   if (a.T <= ST_T) return launch_stream<FP8>(a, st);
-  if (slabs_pay(a.T, a.d_in, a.d_out, FP8, a.cus)) {
-    const SlabPlan p = slab_plan(a.T, a.d_in, a.d_out, a.n_agents, FP8, a.cus);
+  if (slabs_pay(a.T, a.d_in, a.d_out, a.n_agents, a.rank, FP8, a.cus)) {
+    const SlabPlan p = slab_plan(a.T, a.d_in, a.d_out, a.n_agents, a.rank, FP8, a.cus);
     if (const hipError_t e = launch_slabs<FP8>(a, p, st)) return e;
     return launch_join(a, p, st);
   }
@@ -1342,6 +1363,7 @@ hipError_t launch(const ProjectArgs& a, hipStream_t st) {
     SlabPlan p{};
     p.n_tt = 1;
     p.ksa = ksa;
+    p.turns = slab_turns(a.n_agents, a.rank, 2 * a.cus, (a.T + SL_T - 1) / SL_T * ksa);
     if (const hipError_t e = launch_slabs<FP8>(a, p, st)) return e;
   }
   double us;
@@ -1364,8 +1386,8 @@ size_t adapted_projection_bytes(int64_t T, int64_t d_in, int64_t d_out, int n_ag
     size_t b = n_agents > 0 ? (size_t)shrink_slices(T, d_in, rank, cus) * (size_t)T * (size_t)rank * 4 : 0;
     if (T <= ST_T)
       b = plan_bytes(T, rank, stream_plan(T, d_in, d_out, n_agents, fp8, cus));
-    else if (slabs_pay(T, d_in, d_out, fp8, cus))
-      b = plan_bytes(T, rank, slab_plan(T, d_in, d_out, n_agents, fp8, cus));
+    else if (slabs_pay(T, d_in, d_out, n_agents, rank, fp8, cus))
+      b = plan_bytes(T, rank, slab_plan(T, d_in, d_out, n_agents, rank, fp8, cus));
     most = b > most ? b : most;
   }
   return most;
