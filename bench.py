@@ -622,6 +622,104 @@ def fused_projection(prc, w, dev, steps, warmup):
         "lr_cost_in_fused_ms": round(t_fused - t_base, 4)}
 
 
+def layer(prc, w, dev, steps, warmup):
+    """The attention half of a layer with adapters on q and o too, step by step:
+    residual sum and norm, (for a segment) K/V projection with LR rows, q of
+    each row's agent, attention over the shared cache, o, and the next norm in 8
+    bits with the q projection that reads it.  One record for the decode step
+    (a token of each request, each its own agent) and one for a segment of one
+    agent; beside norm, q and o the same in library calls."""
+    import torch
+    torch.cuda.empty_cache()
+    g = torch.Generator(device=dev).manual_seed(8000)
+
+    def nrm(shape, std=1.0):
+        return (torch.randn(*shape, generator=g, device=dev, dtype=torch.float32) * std).to(torch.bfloat16)
+
+    def timed(fn):
+        for _ in range(warmup):
+            fn()
+        torch.cuda.synchronize()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        for _ in range(steps):
+            fn()
+        e1.record()
+        torch.cuda.synchronize()
+        return e0.elapsed_time(e1) / steps
+
+    h, S, d, n_q, n_kv, r, N = w["hidden"], w["S"], w["d"], w["n_q"], w["n_kv"], w["r"], w["N"]
+    nq = n_q * d
+    weight = (1 + nrm((h,), 0.1).float()).to(torch.bfloat16)
+    Wq, Wo, Wkv = nrm((h, nq), h ** -0.5), nrm((nq, h), nq ** -0.5), nrm((h, 2 * n_kv * d), h ** -0.5)
+    A_q, B_q = nrm((h, N * r), h ** -0.5), nrm((N, r, nq), math.sqrt(0.02))
+    A_o, B_o = nrm((nq, N * r), nq ** -0.5), nrm((N, r, h), math.sqrt(0.02))
+    A_kv = nrm((h, 2 * N * r), h ** -0.5)
+    e4m3 = torch.float8_e4m3fn
+    w8s = Wq.float().abs().amax(0) / 448
+    Wq8 = (Wq.float() / w8s).to(e4m3)
+    recs = []
+    for name, T, n_req, kv in (("decode", w["B"], w["B"], S), ("segment", w["seg"], 1, S + w["seg"])):
+        x, res = nrm((T, h)), nrm((T, h))
+        agent = (torch.arange(T, device=dev, dtype=torch.int32) % N) if n_req > 1 else torch.zeros(T, dtype=torch.int32, device=dev)
+        n_tok = T // n_req
+        K, V = nrm((n_req, kv, n_kv, d)), nrm((n_req, kv, n_kv, d))
+        L = nrm((2, N, kv, r))
+        L_k, L_v = (nrm((n_req, kv, r)) for _ in range(2)) if n_req > 1 else (L[0, :1], L[1, :1])
+        B_k, B_v = (nrm((n_req, r, n_kv * d), math.sqrt(0.02)) for _ in range(2))
+        pos = torch.arange(kv - n_tok, kv, dtype=torch.int32, device=dev)[None].expand(n_req, n_tok).contiguous()
+        kvl = torch.full((n_req,), kv, dtype=torch.int32, device=dev)
+        y, s = prc.add_rms_norm(x, weight, res)
+        q = prc.adapted_projection(y, Wq, A_q, B_q, agent)
+        c = dict(Q=q.view(n_req, n_tok, n_q, d), K_base=K, V_base=V, L_k=L_k, L_v=L_v, B_k=B_k, B_v=B_v, positions=pos, kv_len=kvl)
+        O = torch.empty_like(c["Q"])
+        dims = prc.make_dims(c["Q"], K, L_k, L_v, B_k, B_v, w["theta"])
+        ws = torch.empty(max(1, prc.workspace_size(dims)), dtype=torch.uint8, device=dev)
+        pws = torch.empty(max(1, *(prc.adapted_projection_workspace_size(T, a, b, N, r) for a, b in ((h, nq), (nq, h)))),
+                          dtype=torch.uint8, device=dev)
+        o, y2, s2 = torch.empty_like(y), torch.empty(T, h, dtype=e4m3, device=dev), torch.empty_like(s)
+        q8 = torch.empty_like(q)
+        y8, ys, _ = prc.add_rms_norm_fp8(o.zero_(), weight, s)
+        runs = {
+            "norm": lambda: prc.add_rms_norm(x, weight, res, y=y, residual_out=s),
+            "q": lambda: prc.adapted_projection(y, Wq, A_q, B_q, agent, Y=q, workspace=pws),
+            "attention": lambda: attn(prc, c, w["theta"], O, ws),
+            "o": lambda: prc.adapted_projection(O.view(T, nq), Wo, A_o, B_o, agent, Y=o, workspace=pws),
+            "norm_e4m3": lambda: prc.add_rms_norm_fp8(o, weight, s, y=y8, y_scale=ys, residual_out=s2),
+            "q_e4m3": lambda: prc.adapted_projection_fp8(y8, ys, Wq8, w8s, A_q, B_q, agent, Y=q8, workspace=pws),
+        }
+        if n_req == 1:
+            runs["kv"] = lambda: prc.project_kv_and_lr_cache(y, Wkv, A_kv, n_kv, d, 2, N, r, K[0], V[0], L,
+                                                             tok_offset=kv - T, rope_theta=w["theta"])
+
+        def step():
+            for k in ("norm", "kv", "q", "attention", "o"):
+                if k in runs:
+                    runs[k]()
+
+        def plain_norm():
+            t = x.float() + res.float()
+            return (t * torch.rsqrt(t.square().mean(-1, keepdim=True) + 1e-5) * weight.float()).to(torch.bfloat16)
+
+        rows = [(agent == a).nonzero()[:, 0] for a in range(N if n_req > 1 else 1)]
+
+        def plain_q():
+            out = y @ Wq
+            for a, idx in enumerate(rows):
+                out[idx] += (y[idx] @ A_q[:, a * r:(a + 1) * r]) @ B_q[a]
+            return out
+
+        ms = {k: timed(f) for k, f in runs.items()}
+        recs.append({"bench": "layer", "step": name, "rows": T, "requests": n_req, "kv_len": kv, "agents": N, "rank": r,
+                     "ms": {k: round(v, 4) for k, v in ms.items()}, "whole_ms": round(timed(step), 4),
+                     "library_ms": {"norm": round(timed(plain_norm), 4), "q": round(timed(plain_q), 4)},
+                     "q_tflops": round((2 * T * h * nq + 2 * T * r * (h + nq)) / ms["q"] / 1e9, 2),
+                     "q_gbs": round((h * nq + T * (h + nq) + min(N, T) * r * (h + nq)) * 2 / ms["q"] / 1e6, 1),
+                     "norm_gbs": round(4 * T * h * 2 / ms["norm"] / 1e6, 1)})
+        del K, V, L, L_k, L_v, c
+    return recs
+
+
 def paged(prc, w, dev, steps, warmup):
     """The step's decode, prefill and segment projection over paged caches
     (pools of fixed-size blocks in a random order, reached through block
@@ -1067,6 +1165,10 @@ def main():
     ap.add_argument("--paged", action="store_true",
                     help="instead of the step: decode, prefill and segment projection over paged (block-table) "
                          "caches, against the same calls over contiguous caches")
+    ap.add_argument("--layer", action="store_true",
+                    help="instead of the step: the attention half of a layer with adapters on q and o as well "
+                         "(norm, projections of each row's agent, attention, o, the next norm in 8 bits), a decode "
+                         "step and a segment")
     ap.add_argument("--workload", type=int, choices=(2, 4, 5), default=None,
                     help="instead of the step: precompute, prefill and decode at the 8k-context 8B-shaped (2) or "
                          "64k-context 14B-shaped rank-64 (4) workload, against materialise-then-attend")
@@ -1096,6 +1198,10 @@ def main():
         return
     if args.paged:
         for rec in paged(prc, w, dev, args.steps, args.warmup):
+            print(json.dumps(rec), flush=True)
+        return
+    if args.layer:
+        for rec in layer(prc, w, dev, args.steps, args.warmup):
             print(json.dumps(rec), flush=True)
         return
     if args.workload == 5:
