@@ -74,7 +74,8 @@ const char* prc_version(void);
  * also verifies, on the device, before launching an attention or
  * materialise call, that 1 <= kv_len[b] <= s_cap and 0 <= positions[b][i] <
  * kv_len[b] (Sec. 2.2: every query sees a non-empty causal prefix of the
- * cache), and before an adapted projection that agent[i] < n_agents.  It reads the verdict back, so each such call waits for its stream
+ * cache), and before an adapted projection that agent[i] < n_agents.  It reads
+ * the verdict back, so each such call waits for its stream
  * (not usable under graph capture), and on a violation it launches nothing,
  * returns PRC_EDEVDATA and names the first offender (lowest request, then
  * lowest token; a kv_len fault before a position fault) in prc_last_error(). */
@@ -397,7 +398,8 @@ prc_status materialize_agent_kv(const lrsa_dims* dims, const uint16_t* K_base,
  * rounded once (the norm is that of s, not of its rounding).  A row with a NaN
  * or an infinity gives what these formulas give in fp32.
  * Requires d % 8 == 0, 8 <= d <= 65536, row strides >= d and multiples of 8,
- * eps >= 0 and finite, T < 2^31, and outputs that overlap no input and each
+ * eps >= 0 and finite, T < 2^31, T times each row stride at most 2^44
+ * (PRC_EUNSUPPORTED otherwise), and outputs that overlap no input and each
  * other nowhere (but for the rows in place above).  T == 0 is a no-op.
  */
 prc_status add_rms_norm(const uint16_t* x, int64_t T, int64_t d, int64_t ld_x, const uint16_t* residual,

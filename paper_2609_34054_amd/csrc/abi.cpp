@@ -795,6 +795,7 @@ prc_status norm_impl(const char* who, const uint16_t* x, int64_t T, int64_t d, i
   for (const auto& l : lds) {
     if (!l.used) continue;
     if (l.ld < d || l.ld >= (1LL << 40)) return fail(PRC_ESHAPE, "%s=%lld outside [d=%lld, 2^40)", l.name, (long long)l.ld, (long long)d);
+    if (T > 0 && l.ld > (1LL << 44) / T) return fail(PRC_EUNSUPPORTED, "T=%lld rows of %s=%lld are too many", (long long)T, l.name, (long long)l.ld);
     if (l.ld % l.step) return fail(PRC_EALIGN, "%s=%lld is not a multiple of %d elements", l.name, (long long)l.ld, l.step);
   }
   if (T == 0) return ok();

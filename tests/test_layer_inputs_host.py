@@ -55,6 +55,12 @@ def test_8_bit_projection_rejects(kw, code):
     assert prc.lib().prc_last_error().decode()
 
 
+@pytest.mark.parametrize("kw", [dict(ldx=1 << 36), dict(ldr=1 << 36), dict(ldo=1 << 36), dict(ldy=1 << 36)])
+def test_norm_rejects_rows_beyond_64_bit_offsets(kw):
+    assert _norm(T=(1 << 31) - 1, **kw) == EUNSUP
+    assert "too many" in prc.lib().prc_last_error().decode()
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(T=-1), EINVAL), (dict(T=1 << 31), EINVAL), (dict(d=0), EUNSUP), (dict(d=252), EUNSUP), (dict(d=65544), EUNSUP),
     (dict(eps=-1.0), EINVAL), (dict(eps=float("nan")), EINVAL), (dict(eps=float("inf")), EINVAL), (dict(ldx=248), ESHAPE),
