@@ -10,6 +10,7 @@ fails.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib
 import os
@@ -158,6 +159,13 @@ def _raw_stream(stream) -> int:
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _allocating_on(stream):
+    """Tensors made inside belong to `stream`: memory that its earlier work, and no other stream's, may still use."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
 
 
 def _on_gpu(t) -> bool:
@@ -613,12 +621,14 @@ def _norm(func, x, weight, residual, eps, y, y_scale, residual_out, fp8, stream)
     kind = torch.float8_e4m3fn if fp8 else torch.bfloat16
     if _on_gpu(x) and x.dim() == 2:
         nat = _native()
-        if y is None:
-            y = torch.empty(x.shape, dtype=kind, device=x.device)
-        if fp8 and y_scale is None:
-            y_scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-        if residual is not None and residual_out is None:
-            residual_out = torch.empty_like(residual, memory_format=torch.contiguous_format)
+        if y is None or (fp8 and y_scale is None) or (residual is not None and residual_out is None):
+            with _allocating_on(stream):
+                if y is None:
+                    y = torch.empty(x.shape, dtype=kind, device=x.device)
+                if fp8 and y_scale is None:
+                    y_scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+                if residual is not None and residual_out is None:
+                    residual_out = torch.empty_like(residual, memory_format=torch.contiguous_format)
         st = nat.m.norm(getattr(nat, func), fp8, x, weight, residual, eps, residual_out, y, y_scale,
                         torch._C._cuda_getDevice(), _raw_stream(stream))
         if st is not None:
@@ -630,12 +640,13 @@ def _norm(func, x, weight, residual, eps, y, y_scale, residual_out, fp8, stream)
     _rows("weight", weight, torch.bfloat16, (d,))
     if residual is not None:
         _rows("residual", residual, torch.bfloat16, (T, d))
-    if y is None:
-        y = torch.empty((T, d), dtype=kind, device=x.device)
-    if fp8 and y_scale is None:
-        y_scale = torch.empty(T, dtype=torch.float32, device=x.device)
-    if residual is not None and residual_out is None:
-        residual_out = torch.empty((T, d), dtype=torch.bfloat16, device=x.device)
+    with _allocating_on(stream):
+        if y is None:
+            y = torch.empty((T, d), dtype=kind, device=x.device)
+        if fp8 and y_scale is None:
+            y_scale = torch.empty(T, dtype=torch.float32, device=x.device)
+        if residual is not None and residual_out is None:
+            residual_out = torch.empty((T, d), dtype=torch.bfloat16, device=x.device)
     _rows("y", y, kind, (T, d))
     if fp8:
         _rows("y_scale", y_scale, torch.float32, (T,))
@@ -657,6 +668,7 @@ def add_rms_norm(x, weight, residual=None, *, eps: float = 1e-5, y=None, residua
     ``x, residual [T, d]`` (row strides may exceed d) and ``weight [d]`` bf16.
     Returns ``(y, residual_out)``, ``residual_out`` holding s (None without a
     residual, unless one is given to write to; it may be ``residual`` itself).
+    What the call allocates belongs to ``stream``.
     """
     y, _, out = _norm("add_rms_norm", x, weight, residual, eps, y, None, residual_out, False, stream)
     return y, out
@@ -680,13 +692,15 @@ def _adapted(func, X, x_scale, W, w_scale, A_stack, B, agent, Y, workspace, stre
         nat = _native()
         out, ws, raw = Y, workspace, _raw_stream(stream)
         if out is None:
-            out = torch.empty((X.shape[0], W.shape[1]), dtype=torch.bfloat16, device=X.device)
+            with _allocating_on(stream):
+                out = torch.empty((X.shape[0], W.shape[1]), dtype=torch.bfloat16, device=X.device)
         while True:
             st = nat.m.adapted(getattr(nat, func), nat.adapted_projection_workspace_size, fp8, X, x_scale, W, w_scale,
                                A_stack, B, agent, out, ws, torch._C._cuda_getDevice(), raw)
             if type(st) is not tuple:
                 break
-            ws = torch.empty(st[0], dtype=torch.uint8, device=X.device)
+            with _allocating_on(stream):
+                ws = torch.empty(st[0], dtype=torch.uint8, device=X.device)
         if st is not None:
             if st:
                 _check(func, st)
@@ -712,7 +726,8 @@ def _adapted(func, X, x_scale, W, w_scale, A_stack, B, agent, Y, workspace, stre
         _rows("A_stack", A_stack, torch.bfloat16, (d_in, n_agents * rank), contiguous=True)
         _rows("agent", agent, torch.int32, (T,))
     if Y is None:
-        Y = torch.empty((T, d_out), dtype=torch.bfloat16, device=X.device)
+        with _allocating_on(stream):
+            Y = torch.empty((T, d_out), dtype=torch.bfloat16, device=X.device)
     _rows("Y", Y, torch.bfloat16, (T, d_out))
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
@@ -721,7 +736,8 @@ def _adapted(func, X, x_scale, W, w_scale, A_stack, B, agent, Y, workspace, stre
     with torch.cuda.device(dev):
         need = adapted_projection_workspace_size(T, d_in, d_out, n_agents, rank)
         if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+            with _allocating_on(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
         tail = [_ptr(A_stack), _ptr(B), n_agents, rank, _ptr(agent), _ptr(Y), _ld(Y), _ptr(workspace), ws_bytes,
                 _stream(stream)]

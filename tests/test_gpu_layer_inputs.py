@@ -293,6 +293,27 @@ def test_side_stream_and_graphs(T):
             assert torch.equal(Y, want[i]) and torch.equal(y, wy) and torch.equal(out, ws_), (rep, i)
 
 
+@pytest.mark.parametrize("raw", [False, True])
+@pytest.mark.parametrize("T", [8, 300])
+def test_what_a_call_allocates_belongs_to_its_stream(T, raw):
+    """Memory that pending work of the current stream still writes is not handed to a call on another stream."""
+    c, nrm = project_case(T, T, 512, 528, 4, 16, "mixed"), norm_case(T, 512, True)
+    want, (wy, wr) = call(prc, c), prc.add_rms_norm(*nrm)
+    size = prc.adapted_projection_workspace_size(T, 512, 528, 4, 16)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    bufs = [torch.empty(b, dtype=torch.uint8, device="cuda") for b in (size, 2 * T * 528, 2 * T * 512, 2 * T * 512)]
+    torch.cuda._sleep(20_000_000)
+    for b in bufs:
+        b.fill_(255)
+    del bufs, b
+    st = side.cuda_stream if raw else side
+    got = call(prc, c, stream=st)
+    y, r = prc.add_rms_norm(*nrm, stream=st)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(y, wy) and torch.equal(r, wr)
+
+
 def test_native_and_python_marshalling_agree(monkeypatch):
     from paper_2609_34054_amd import binding
     c, c8 = project_case(9, 20, 256, 272, 3, 16), project_case(9, 20, 256, 272, 3, 16, fp8=True)
