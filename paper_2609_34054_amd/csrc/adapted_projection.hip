@@ -1271,7 +1271,9 @@ hipError_t launch_mid(const ProjectArgs& a, int ksa, hipStream_t st) {
 
 // The time of slabs in `ks` slices, in microseconds: a stage takes 0.29 while a CU
 // has one workgroup and 0.56 with two (96 rows of 4096 x 4096 in bf16: one slice,
-// on half the CUs, 27.3 us, three 19.1; four, which do not run at once, 24.2), the
+// on half the CUs, 27.3 us, three 19.1; four, which do not run at once, 24.2), 1.8
+// times that in e4m3 if W's rows start inside 128-byte lines (320 rows of 5120 x
+// 7248: 55 us, as tiles 45; in bf16 664 rows of 1232 x 496 17.2 and 23.6), the
 // stages together no less than W takes at the rate of a copy (24 rows of 4096 x
 // 14336: one slice 30.5 us, two 36.7); sums are written and read at 3.5 TB/s (256
 // rows of 1024 x 1024: three slices 10.8 us, seven 13.9), each row's B at 11.
@@ -1279,7 +1281,7 @@ double slab_time(int64_t T, int64_t d_in, int64_t d_out, int rank, bool fp8, int
   const int64_t cw = fp8 ? 128 : 64, n = ((d_out + cw - 1) / cw + 1) * ((T + SL_T - 1) / SL_T) * ks, nk = (d_in + cw - 1) / cw;
   const int64_t rounds = (n + 2 * cus - 1) / (2 * cus);
   const double fill = n < cus ? 1.0 : (rounds > 1 ? 2.0 : (double)n / cus), out = (double)T * (double)d_out;
-  const double stages = (double)(rounds * ((nk + ks - 1) / ks)) * (0.29 + 0.27 * (fill - 1.0));
+  const double stages = (double)(rounds * ((nk + ks - 1) / ks)) * (0.29 + 0.27 * (fill - 1.0)) * (fp8 && d_out % cw != 0 ? 1.8 : 1.0);
   const double once = (double)d_in * (double)d_out * (fp8 ? 1.0 : 2.0) / 5e6;
   return 7.5 + (stages > once ? stages : once) + out * 8.0 * ks / 3.5e6 + out * 2.0 * rank / 11e6;
 }
@@ -1337,9 +1339,9 @@ int tile_form(int64_t T, int64_t d_in, int64_t d_out, int n_agents, bool fp8, in
 // once more.  Measured for 96 to 512 rows of 1024 x 1024 to 14336 x 4096 and 4096
 // x 14336, in bf16 with rank 16 and e4m3 with rank 64: 4096 x 4096, 96 rows 19.1
 // us as slabs against 29.2, 512 rows 57.8 against 34.4; 14336 x 4096 in e4m3, 160
-// rows 35.6 against 61.9.  Up to 64 rows always: less than a tile's.  Without adapters
+// rows 35.6 against 61.9; 1100 rows of 4096 x 256 21.6 against 40.1.  Up to 64 rows always: less than a tile's.  Without adapters
 // (n_agents 0) it goes as with some of rank 16.
-constexpr int SL_MOST = 1024;  // bounds the workspace
+constexpr int SL_MOST = 4096;  // bounds the workspace
 
 bool slabs_pay(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, bool fp8, int cus) {
   if (T <= SL_T || T > SL_MOST) return T <= SL_T;
