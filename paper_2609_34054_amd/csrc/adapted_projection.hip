@@ -386,8 +386,11 @@ __global__ void __launch_bounds__(512, 4) slab_kernel(const ProjectArgs a, const
   const int m = ad ? L - 8 * per : L % 8 * per + L / 8;
   if (!ad && m >= n_main) return;  // uniform over the workgroup
   const int ks = ad ? p.ksa : p.ks;
-  const int tt = __builtin_amdgcn_readfirstlane(ad ? m / p.turns / p.ksa : m % p.n_tt), ct = ad ? 0 : m / p.n_tt % p.n_ct;
-  const int ki = __builtin_amdgcn_readfirstlane(ad ? m / p.turns % p.ksa : m / p.n_tt / p.n_ct);
+  // First turns first, so that those of workgroups without an agent delay none
+  // (2048 rows of 5120 x 5120 in e4m3, rank 64: 75.8 us turns inside, 70.7).
+  const int n_rt = (int)((a.T + SL_T - 1) / SL_T) * p.ksa, mt = ad ? m % n_rt : 0;
+  const int tt = __builtin_amdgcn_readfirstlane(ad ? mt / p.ksa : m % p.n_tt), ct = ad ? 0 : m / p.n_tt % p.n_ct;
+  const int ki = __builtin_amdgcn_readfirstlane(ad ? mt % p.ksa : m / p.n_tt / p.n_ct);
   const int64_t t0 = (int64_t)tt * SL_T;
   const int toks = (int)(a.T - t0 < SL_T ? a.T - t0 : (int64_t)SL_T), d_in = (int)a.d_in;
   const int nk = (d_in + C::KS - 1) / C::KS;
@@ -506,7 +509,7 @@ __global__ void __launch_bounds__(512, 4) slab_kernel(const ProjectArgs a, const
       id[b] = todo != 0 ? __builtin_amdgcn_readlane(ag, __builtin_ctzll(todo)) : -1;
       if (todo != 0) todo &= ~__ballot(ag == id[b]);
     }
-    if (turn % p.turns != m % p.turns) continue;  // uniform
+    if (turn % p.turns != m / n_rt) continue;  // uniform
 #pragma unroll
     for (int j = 0; j < C::NA; ++j) {
       const int k = (8 * j + wv) * 8 + lane / 8, blk = (lane % 8 / 2) ^ swz<false>(k), c = blk * 16 % rp + lane % 2 * 8;

@@ -160,7 +160,7 @@ def test_projection_tile_shapes(T, k, n, N, r, order, fp8):
 # A few hundred rows as 64-row slabs: one and several k slices, ends inside a slab, a stage and 16 columns; more
 # agents among 64 rows than are taken at once; 128 x 64 tiles where there are too many slabs.
 SHAPES_SLABS = [(17, 136, 72), (47, 4112, 272), (64, 64, 4096), (66, 1032, 3080), (191, 2056, 1032), (257, 5128, 520),
-                (1000, 1096, 200), (1024, 72, 1048), (300, 3592, 4096), (90, 520, 40000)]
+                (1000, 1096, 200), (1024, 72, 1048), (300, 3592, 4096), (90, 520, 40000), (1100, 1032, 136), (4090, 520, 64)]
 
 
 @pytest.mark.parametrize("fp8", [False, True])
