@@ -67,7 +67,7 @@ __device__ __forceinline__ u32x4 bf16_of_e4m3(u32x2 v) {
 // sums are added through LDS in a fixed order and go to the workspace; a
 // second kernel adds the k slices and the expanded adapter rows.
 //
-// 4096 x 4096 in bf16, one row: 11.9 us for both kernels, of which the weights
+// 4096 x 4096 in bf16, one row: 11.0 us for both kernels, of which the weights
 // (32 MB) take 6.7 at the rate of a copy; the rest is two launches and the start
 // and end of the ring.  With more than 16 rows their loads and MFMAs, repeated
 // for each distinct agent, outweigh the barriers saved (see the slabs below).
@@ -230,7 +230,8 @@ __global__ void __launch_bounds__(ST_W * 64) stream_kernel(const ProjectArgs a, 
 }
 
 // Y of 256 columns of a row, four columns a lane: each of four waves takes a
-// quarter of the ranks and every fourth k slice, all its loads in flight at once
+// quarter of the ranks and every fourth k slice, its loads in flight together (8 x
+// 5120 x 5120 in e4m3, rank 64: 14.6 -> 13.8 us for the two kernels)
 // (lanes past the last column read the row's first ones); their sums are added
 // in a fixed order.
 template <int R>
@@ -248,7 +249,15 @@ __global__ void __launch_bounds__(256) join_kernel(const ProjectArgs a, const Sl
   f32x4 wsc = {1.f, 1.f, 1.f, 1.f};
   if (a.x_scale != nullptr) wsc = *reinterpret_cast<const f32x4*>(a.w_scale + c) * xs;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int k = w; k < p.ks; k += 4) v += *reinterpret_cast<const f32x4*>(P + (k * T + t) * a.d_out + c);
+  for (int k = w; k < p.ks; k += 16) {
+    f32x4 u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (k + 4 * i < p.ks) u[i] = *reinterpret_cast<const f32x4*>(P + ((k + 4 * i) * T + t) * a.d_out + c);
+    }
+    v += (u[0] + u[1]) + (u[2] + u[3]);
+  }
   v *= wsc;
   if (lr) {
     u32x2 b[RW];
@@ -257,7 +266,13 @@ __global__ void __launch_bounds__(256) join_kernel(const ProjectArgs a, const Sl
     for (int j = 0; j < RW; ++j) b[j] = *reinterpret_cast<const u32x2*>(B + j * a.d_out);
     const float* H = P + p.h_at + t * R + w * RW + lane % RW;
     float h = 0.f;
-    for (int k = 0; k < p.ksa; ++k) h += H[k * T * R];
+    for (int k = 0; k < p.ksa; k += 8) {
+      float u[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = k + i < p.ksa ? H[(k + i) * T * R] : 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h += u[i];
+    }
     const float hb = bf_lo(pack_bf16(h * xs, 0.f));
 #pragma unroll
     for (int j = 0; j < RW; ++j) {
