@@ -249,6 +249,24 @@ def test_projection_gives_the_same_bits_again(T, fp8):
         assert torch.equal(call(prc, c), want)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T", [3, 40])
+def test_projection_among_very_many_adapters(T, fp8):
+    """Rows of A of 32 MB (offsets of a stage's rows past d_in exceed 32 bits): the bits of a call that has only the
+    adapters in use."""
+    k, n, N, r = 16, 32, 1 << 18, 64
+    c = project_case(T, T, k, n, T, r, "mixed", fp8)
+    c["agent"] = torch.arange(T, dtype=torch.int32, device="cuda").flip(0)
+    where = (torch.arange(T, device="cuda") * (N - 1)) // (T - 1)
+    A = torch.full((k, N, r), float("nan"), dtype=BF, device="cuda")
+    B = torch.full((N, r, n), float("nan"), dtype=BF, device="cuda")
+    A[:, where], B[where] = c["A_stack"].view(k, T, r), c["B"]
+    many = dict(c, A_stack=A.view(k, N * r), B=B, agent=where[c["agent"].long()].int())
+    want = call(prc, c)
+    check_project(want, *ref_of(c))
+    assert torch.equal(call(prc, many), want)
+
+
 def test_projection_of_no_rows():
     c = project_case(1, 0, 64, 48, 2, 8)
     assert call(prc, c).shape == (0, 48)
