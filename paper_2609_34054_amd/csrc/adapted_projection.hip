@@ -2,8 +2,10 @@
 // (Eq. 1 for many agents at once):
 //     Y[i] = X[i] W + (X[i] A_a) B_a,   a = agent[i]   (no such agent: X[i] W)
 // in bf16, or with X and W in e4m3 (X = x_scale[i] X8, W = w_scale[j] W8).
-// The rank-r rows X A_a are formed first (fp32 sums, then bf16, as the LR
-// caches hold them) and added, expanded by B_a, as Y is written.
+// The rank-r rows X A_a are formed first, in fp32, and added, expanded by B_a, as
+// Y is written: by fp32 products for few rows, for tiles by matrix instructions
+// that take each row as the sum of two bf16 ones, 16 bits of it (one alone made
+// the error of Y 6 to 11% larger at ranks 8 and 16 and 25 to 28% at rank 64).
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -273,10 +275,10 @@ __global__ void __launch_bounds__(256) join_kernel(const ProjectArgs a, const Sl
 #pragma unroll
       for (int i = 0; i < 8; ++i) h += u[i];
     }
-    const float hb = bf_lo(pack_bf16(h * xs, 0.f));
+    h *= xs;
 #pragma unroll
     for (int j = 0; j < RW; ++j) {
-      const float hj = readlane_f(hb, j);
+      const float hj = readlane_f(h, j);
       v[0] += hj * bf_lo(b[j][0]);
       v[1] += hj * bf_hi(b[j][0]);
       v[2] += hj * bf_lo(b[j][1]);
@@ -625,16 +627,34 @@ __device__ __forceinline__ void scale_tile(const ProjectArgs& a, f32x16 (&acc)[C
 }
 
 // The expanded adapter rows: all waves of the tile (TT tokens from t0, NP column
-// blocks from c0) together, four of its agents at a time.  The tile's rows X A_a
-// are summed over the k slices, rounded to bf16 and put into LDS, and each
-// agent's rows of B_a beside them, laid out as the weights are.  A product
-// is added to the tokens of its agent alone, so that what is infinite
-// or NaN in an adapter stays in the rows that use it.  2048 x 5120 x 5120 in e4m3,
-// rank 64: 14 us of the tiles' 59, of which the sums' loads 6 and the MFMAs 2.5.
+// blocks from c0) together, four of its agents at a time (three where LDS holds no
+// more).  The tile's rows X A_a are summed over the k slices, split into two bf16
+// parts and put into LDS, and each agent's rows of B_a beside them, laid out as
+// the weights are.  A product is added to the tokens of its agent alone, so that
+// what is infinite or NaN in an adapter stays in the rows that use it.  The second
+// part costs 4096 x 4096 x 4096 in bf16 of runs nothing at rank 16 and 8 of 159 us
+// at rank 64, 2048 x 5120 x 5120 in e4m3, rank 64, 0.6 of 67.5.
 constexpr int EX_A = 4;  // agents at a time
+constexpr int EX_LDS = 160 * 1024;
 
 template <int NP, int TT>
-constexpr int expand_bytes = TT * 128 + EX_A * 64 * NP * 64;
+constexpr int expand_agents(int rp) {  // of (padded) rank rp
+  return (EX_LDS - TT * 256) / (rp * NP * 64) < EX_A ? (EX_LDS - TT * 256) / (rp * NP * 64) : EX_A;
+}
+template <int NP, int TT>
+constexpr int expand_bytes = TT * 256 + expand_agents<NP, TT>(64) * 64 * NP * 64;
+
+// v = hi + lo as bf16, to 2^-17 of it.  An infinity (or NaN) is hi's alone.
+__device__ __forceinline__ void split_bf16(f32x4 v0, f32x4 v1, u32x4& hi, u32x4& lo) {
+  hi = u32x4{pack_bf16(v0[0], v0[1]), pack_bf16(v0[2], v0[3]), pack_bf16(v1[0], v1[1]), pack_bf16(v1[2], v1[3])};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float a = j < 2 ? v0[2 * j] : v1[2 * j - 4], b = j < 2 ? v0[2 * j + 1] : v1[2 * j - 3];
+    const uint32_t ha = hi[j] << 16, hb = hi[j] & 0xffff0000u;
+    lo[j] = pack_bf16((ha & 0x7f800000u) == 0x7f800000u ? 0.f : a - __uint_as_float(ha),
+                      (hb & 0x7f800000u) == 0x7f800000u ? 0.f : b - __uint_as_float(hb));
+  }
+}
 
 template <bool FP8, int NP, int TT, int CB, int TB>
 __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x16 (&acc)[CB][TB], char* lds, int64_t t0, int tw,
@@ -659,6 +679,7 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
   auto chunk = [&](int r, int c) {  // where chunk c of row r lies
     return r * rp * 2 + (nc == 2 ? c : (nc == 4 ? c ^ ((r >> 2) & 3) : c ^ ((r >> 1) & 7))) * 16;
   };
+  constexpr int part = TT * 128;  // the rows' low parts lie this far behind (room for rank 64)
   auto rows_to_lds = [&]() {
     // 16-byte chunk u of the tile's rows is thread u % 512's, two at a time.
     const float* H = static_cast<const float*>(a.ws) + t0 * R;
@@ -691,21 +712,24 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
           v[i][0] *= xsc;
           v[i][1] *= xsc;
         }
-        *reinterpret_cast<u32x4*>(lds + chunk(u / nc, u % nc)) =
-            u32x4{pack_bf16(v[i][0][0], v[i][0][1]), pack_bf16(v[i][0][2], v[i][0][3]), pack_bf16(v[i][1][0], v[i][1][1]),
-                  pack_bf16(v[i][1][2], v[i][1][3])};
+        u32x4 hi, lo;
+        split_bf16(v[i][0], v[i][1], hi, lo);
+        *reinterpret_cast<u32x4*>(lds + chunk(u / nc, u % nc)) = hi;
+        *reinterpret_cast<u32x4*>(lds + part + chunk(u / nc, u % nc)) = lo;
       }
     }
   };
   constexpr int WRB = NP * 64;  // bytes of a row of B
-  char* bs = lds + TT * rp * 2;
+  char* bs = lds + 2 * part;
+  static_assert(expand_agents<NP, TT>(32) == EX_A, "fewer at rank 64 alone");
+  const int most = rp == 64 ? expand_agents<NP, TT>(64) : EX_A;
   const int wk = 8 * h + i16 / 4, ws = swz_blocks<false, NP>(wk);
   const int wo = wk * WRB + (grp & 1) * 32 + i16 % 4 * 8;
   for (bool first = true; any != 0; first = false) {
-    int id[EX_A];
+    int id[EX_A] = {-1, -1, -1, -1};
 #pragma unroll
     for (int g = 0; g < EX_A; ++g) {
-      id[g] = -1;
+      if (g >= most) break;
 #pragma unroll
       for (int i = NT - 1; i >= 0; --i)
         if (todo[i] != 0) id[g] = __builtin_amdgcn_readlane(all[i], __builtin_ctzll(todo[i]));
@@ -748,9 +772,12 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
             for (int kk = 0; kk < rp / 16; ++kk) {
               const char* p = bs + g * rp * WRB + wo + ((cb0 + cb) ^ ws) * 64 + 16 * kk * WRB;
               const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * WRB);
-              u32x4 fh = *reinterpret_cast<const u32x4*>(lds + chunk(tw + 32 * tb + l32, 2 * kk + h));
-              if (!mine) fh = u32x4{0u, 0u, 0u, 0u};
-              sum = mfma32x32x16(as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]}), as_bf16x8(fh), sum);
+              const char* hp = lds + chunk(tw + 32 * tb + l32, 2 * kk + h);
+              u32x4 fh = *reinterpret_cast<const u32x4*>(hp), fl = *reinterpret_cast<const u32x4*>(hp + part);
+              if (!mine) fh = fl = u32x4{0u, 0u, 0u, 0u};
+              const bf16x8 fb = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
+              sum = mfma32x32x16(fb, as_bf16x8(fl), sum);
+              sum = mfma32x32x16(fb, as_bf16x8(fh), sum);
             }
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[cb][tb][j] = whole ? sum[j] : (mine ? acc[cb][tb][j] + sum[j] : acc[cb][tb][j]);
@@ -758,42 +785,45 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
         }
         continue;
       }
-      bool mine[TB];
-      uint64_t some = 0;
-#pragma unroll
-      for (int tb = 0; tb < TB; ++tb) {
-        mine[tb] = ag[tb] == id[g];
-        some |= __ballot(mine[tb]);
-      }
-      if (some == 0) continue;  // uniform
+      // Addresses formed anew for each agent: those of all, kept, spill.
+      int r0 = tw + l32, w0 = wo;
+      asm volatile("" : "+v"(r0), "+v"(w0));
       auto add = [&](auto KR) {  // KR steps of 16 ranks
         constexpr int kr = decltype(KR)::value;
-        bf16x8 fh[TB][kr];
+        const char* rows = lds + r0 * kr * 32;  // rows 32 further swizzle alike
+        const int hs = (kr == 1 ? h : (kr == 2 ? h ^ ((r0 >> 2) & 3) : h ^ ((r0 >> 1) & 7))) * 16;
+        // Both parts of one token block at a time: those of all spill.
 #pragma unroll
-        for (int kk = 0; kk < kr; ++kk)
-#pragma unroll
-          for (int tb = 0; tb < TB; ++tb)
-            fh[tb][kk] = as_bf16x8(*reinterpret_cast<const u32x4*>(lds + chunk(tw + 32 * tb + l32, 2 * kk + h)));
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-          const char* p = bs + g * rp * WRB + wo + ((cb0 + cb) ^ ws) * 64;
-          bf16x8 fb[kr];
+        for (int tb = 0; tb < TB; ++tb) {
+          const bool mine = ag[tb] == id[g];
+          if (__ballot(mine) == 0) continue;  // uniform
+          bf16x8 fh[kr], fl[kr];
 #pragma unroll
           for (int kk = 0; kk < kr; ++kk) {
-            const u32x2 lo = lds_read_tr16(p + 16 * kk * WRB), hi = lds_read_tr16(p + (16 * kk + 4) * WRB);
-            fb[kk] = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
+            const char* p = rows + 32 * tb * kr * 32 + (hs ^ (32 * kk));  // chunk 2 kk + h
+            fh[kk] = as_bf16x8(*reinterpret_cast<const u32x4*>(p));
+            fl[kk] = as_bf16x8(*reinterpret_cast<const u32x4*>(p + part));
           }
 #pragma unroll
-          for (int tb = 0; tb < TB; ++tb) {
+          for (int cb = 0; cb < CB; ++cb) {
+            const char* p = bs + g * rp * WRB + w0 + ((cb0 + cb) ^ ws) * 64;
+            bf16x8 fb[kr];
+#pragma unroll
+            for (int kk = 0; kk < kr; ++kk) {
+              const u32x2 lo = lds_read_tr16(p + 16 * kk * WRB), hi = lds_read_tr16(p + (16 * kk + 4) * WRB);
+              fb[kk] = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
+            }
             f32x16 sum;
 #pragma unroll
             for (int j = 0; j < 16; ++j) sum[j] = 0.f;
 #pragma unroll
-            for (int kk = 0; kk < kr; ++kk) sum = mfma32x32x16(fb[kk], fh[tb][kk], sum);
+            for (int kk = 0; kk < kr; ++kk) sum = mfma32x32x16(fb[kk], fl[kk], sum);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) acc[cb][tb][j] += mine[tb] ? sum[j] : 0.f;
+            for (int kk = 0; kk < kr; ++kk) sum = mfma32x32x16(fb[kk], fh[kk], sum);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[cb][tb][j] += mine ? sum[j] : 0.f;
+            __builtin_amdgcn_sched_barrier(0);
           }
-          __builtin_amdgcn_sched_barrier(0);
         }
       };
       if (rp == 16) add(std::integral_constant<int, 1>{});
@@ -856,7 +886,8 @@ struct Tile {
   // the others, so that every wave's count is known to the compiler (what
   // exceeds NW loads zeros past the rings).
   static constexpr int NW = WB / 1024, N0 = (NW + 7) / 8, N1 = (NW - 4 * N0 + 3) / 4;
-  static constexpr int RINGS = 3 * XB + 4 * WB, BYTES = RINGS + (4 * (N0 + N1) > NW ? 1024 : 0);
+  static constexpr int RINGS = 3 * XB + 4 * WB, LOADS = RINGS + (4 * (N0 + N1) > NW ? 1024 : 0);
+  static constexpr int BYTES = LOADS > expand_bytes<NP, TL_T> ? LOADS : expand_bytes<NP, TL_T>;
 };
 
 // One wave's part of a tile: tokens t0 + 64 wt .., columns c0 + 32 cb0 .. of CB

@@ -1,0 +1,41 @@
+"""Adapted projections of whole numbers, whose results are exact: compared bit for bit."""
+import pytest
+import torch
+
+from layer_input_exact import exact_case, exact_y
+from layer_input_ref import call
+import paper_2609_34054_amd as prc
+
+pytestmark = pytest.mark.gpu
+
+# One of each form and tile shape: rows streamed, slabs, tiles of 128 x 64 to 256 x 256; ends inside tiles.
+FORMS = [(1, 1032, 264), (16, 528, 144), (40, 1040, 272), (100, 2064, 1040), (1000, 1024, 4096), (2500, 1040, 2064),
+         (2040, 272, 5120), (2040, 528, 6144), (4090, 272, 4080), (3000, 528, 4096)]
+
+
+def check(c):
+    got, want = call(prc, c), exact_y(c)
+    wrong = (got.double() != want).nonzero()
+    assert not len(wrong), (len(wrong), wrong[0].tolist(), float(got[tuple(wrong[0])]), float(want[tuple(wrong[0])]))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,k,n", FORMS)
+def test_adapter_rows_keep_their_bits(T, k, n, fp8):
+    """Entries of X A_a of 14 bits that cancel in Y."""
+    k, n = ((k + 15) // 16 * 16, (n + 15) // 16 * 16) if fp8 else (k, n)
+    for r, N in ((8, 3), (16, 1), (32, 12), (64, 9)):
+        print(f"project {T} {k} {n} {N} r{r} fp8={fp8}", flush=True)
+        check(exact_case(T + k + r, T, k, n, N, r, fp8, wide=True))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T", [3, 40, 1000])
+def test_an_infinite_adapter_row_is_infinite(T, fp8):
+    """Not NaN: a row of X A_a that is infinite, times one."""
+    c = exact_case(T, T, 1024, 4096, 2, 16, fp8, device="cuda")
+    c["agent"].fill_(1)
+    c["B"].zero_()
+    c["B"][1] = 1.0
+    c["A_stack"][1023, 16 + 5] = float("inf")   # X is 1 there in every row
+    assert (call(prc, c) == float("inf")).all()
