@@ -138,13 +138,26 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rms_norm_kernel(const N
   }
 }
 
+// A grid holds fewer than 2^32 threads: what is longer goes in launches of 2^31
+// (2^25 rows up to 512 wide, 2^23 to 4096, 2^21 past 8192).
 template <int TPR, int NCH>
 hipError_t launch(const NormArgs& a, hipStream_t st) {
-  const int rpw = TPR < 256 ? 256 / TPR : 1, threads = TPR < 256 ? 256 : TPR;
-  const dim3 grid((unsigned)((a.T + rpw - 1) / rpw));
-  if (a.y_scale != nullptr) hipLaunchKernelGGL((rms_norm_kernel<TPR, NCH, true>), grid, dim3(threads), 0, st, a);
-  else hipLaunchKernelGGL((rms_norm_kernel<TPR, NCH, false>), grid, dim3(threads), 0, st, a);
-  return hipGetLastError();
+  constexpr int rpw = TPR < 256 ? 256 / TPR : 1, threads = TPR < 256 ? 256 : TPR;
+  constexpr int64_t most = (1LL << 31) / threads * rpw;
+  for (int64_t r = 0; r < a.T; r += most) {
+    NormArgs p = a;
+    p.T = a.T - r < most ? a.T - r : most;
+    p.x = a.x + r * a.ld_x;
+    if (a.residual != nullptr) p.residual = a.residual + r * a.ld_res;
+    if (a.residual_out != nullptr) p.residual_out = a.residual_out + r * a.ld_ro;
+    p.y = static_cast<char*>(a.y) + r * a.ld_y * (a.y_scale != nullptr ? 1 : 2);
+    if (a.y_scale != nullptr) p.y_scale = a.y_scale + r;
+    const dim3 grid((unsigned)((p.T + rpw - 1) / rpw));
+    if (a.y_scale != nullptr) hipLaunchKernelGGL((rms_norm_kernel<TPR, NCH, true>), grid, dim3(threads), 0, st, p);
+    else hipLaunchKernelGGL((rms_norm_kernel<TPR, NCH, false>), grid, dim3(threads), 0, st, p);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
