@@ -1435,8 +1435,16 @@ hipError_t launch(const ProjectArgs& a, hipStream_t st) {
 
 }  // namespace
 
-size_t adapted_projection_bytes(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, int cus) {
-  if (n_agents == 0) rank = 8;
+// A grid holds fewer than 2^32 threads, 2^23 workgroups here.  Tiles of 128 x 64 are
+// the most, the adapters' slabs one per 64 rows when rows are many; so a call goes
+// in parts of rows that have about 2^22 such tiles and 2^28 rows at most (64 GB of Y).
+static int64_t rows_at_once(int64_t T, int64_t d_out) {
+  const int64_t across = (d_out + 63) / 64, tiles = (1 << 22) / across;
+  const int64_t most = tiles * 128 < (1LL << 28) ? tiles * 128 : (1LL << 28), parts = (T + most - 1) / most;
+  return parts == 1 ? T : ((T + parts - 1) / parts + 255) / 256 * 256;
+}
+
+static size_t part_bytes(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, int cus) {
   size_t most = 0;
   for (const bool fp8 : {false, true}) {
     size_t b = n_agents > 0 ? (size_t)shrink_slices(T, d_in, rank, cus) * (size_t)T * (size_t)rank * 4 : 0;
@@ -1449,8 +1457,26 @@ size_t adapted_projection_bytes(int64_t T, int64_t d_in, int64_t d_out, int n_ag
   return most;
 }
 
+size_t adapted_projection_bytes(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, int cus) {
+  if (n_agents == 0) rank = 8;
+  const int64_t part = rows_at_once(T, d_out), last = T - (T - 1) / part * part;
+  const size_t a = part_bytes(part, d_in, d_out, n_agents, rank, cus);
+  const size_t b = last == part ? a : part_bytes(last, d_in, d_out, n_agents, rank, cus);
+  return a > b ? a : b;
+}
+
 hipError_t launch_adapted_projection(const ProjectArgs& a, hipStream_t st) {
-  return a.x_scale != nullptr ? launch<true>(a, st) : launch<false>(a, st);
+  const int64_t part = rows_at_once(a.T, a.d_out);
+  for (int64_t r = 0; r < a.T; r += part) {
+    ProjectArgs p = a;
+    p.T = a.T - r < part ? a.T - r : part;
+    p.X = static_cast<const char*>(a.X) + r * a.ld_x * (a.x_scale != nullptr ? 1 : 2);
+    if (a.x_scale != nullptr) p.x_scale = a.x_scale + r;
+    if (a.agent != nullptr) p.agent = a.agent + r;
+    p.Y = a.Y + r * a.ld_y;
+    if (const hipError_t e = a.x_scale != nullptr ? launch<true>(p, st) : launch<false>(p, st)) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace prc

@@ -3,7 +3,8 @@ import pytest
 import torch
 
 import paper_2609_34054_amd as prc
-from layer_input_ref import Draws, check_norm, check_norm_fp8
+from layer_input_exact import exact_case, exact_y
+from layer_input_ref import Draws, call as project, check_norm, check_norm_fp8
 
 pytestmark = pytest.mark.gpu
 BF = torch.bfloat16
@@ -49,3 +50,25 @@ def test_norm_of_more_rows_than_a_grid_holds(T, d, fp8):
         assert same(g, v)
     del long_x, long_res, got
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("T,k,n,r,fp8", [((1 << 29) + 77, 8, 8, 8, False), ((1 << 29) + 77, 16, 16, 8, True),
+                                         ((1 << 20) + 77, 8, (1 << 15) + 64, 16, False)])
+def test_projection_of_more_rows_than_a_grid_holds(T, k, n, r, fp8):
+    print(f"project {T} {k} {n} r{r} fp8={fp8}", flush=True)
+    c = exact_case(T + k, N, k, n, 3, r, fp8)
+    want = exact_y(c).to(BF)
+    assert torch.equal(project(prc, c), want)
+    long = dict(c, X=again(c["X"].view(torch.int8 if fp8 else torch.int16), T).view(c["X"].dtype), agent=again(c["agent"], T))
+    if fp8:
+        long["x_scale"] = again(c["x_scale"], T)
+    assert same(project(prc, long), want)
+    del long
+    torch.cuda.empty_cache()
+
+
+def test_workspace_of_more_rows_than_a_grid_holds():
+    """No larger than the parts it goes in need."""
+    size = prc.adapted_projection_workspace_size
+    assert size((1 << 29) + 77, 8, 8, 3, 8) <= (1 << 28) * 8 * 4
+    assert size((1 << 31) - 1, 64, 8, 3, 64) <= (1 << 28) * 64 * 4
