@@ -45,6 +45,12 @@ __device__ __forceinline__ void wait_loads() {
 }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
+// Four column scales, which need not lie at a multiple of 16 bytes.
+__device__ __forceinline__ f32x4 ld_scales(const float* p) {
+  typedef f32x4 f32x4_at4 __attribute__((aligned(4)));
+  return *reinterpret_cast<const f32x4_at4*>(p);
+}
+
 // Eight e4m3 values as bf16 (exact).
 __device__ __forceinline__ u32x4 bf16_of_e4m3(u32x2 v) {
   u32x4 o;
@@ -249,7 +255,7 @@ __global__ void __launch_bounds__(256) join_kernel(const ProjectArgs a, const Sl
   const bool lr = ag >= 0 && ag < a.n_agents;  // uniform
   const float xs = a.x_scale != nullptr ? a.x_scale[t] : 1.f;
   f32x4 wsc = {1.f, 1.f, 1.f, 1.f};
-  if (a.x_scale != nullptr) wsc = *reinterpret_cast<const f32x4*>(a.w_scale + c) * xs;
+  if (a.x_scale != nullptr) wsc = ld_scales(a.w_scale + c) * xs;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   for (int k = w; k < p.ks; k += 16) {
     f32x4 u[4];
@@ -618,7 +624,7 @@ __device__ __forceinline__ void scale_tile(const ProjectArgs& a, f32x16 (&acc)[C
     for (int jg = 0; jg < 4; ++jg) {
       const int64_t c = cw + 32 * cb + jg * 8 + 4 * h;
       f32x4 wsc = {0.f, 0.f, 0.f, 0.f};
-      if (c < a.d_out) wsc = *reinterpret_cast<const f32x4*>(a.w_scale + c);
+      if (c < a.d_out) wsc = ld_scales(a.w_scale + c);
 #pragma unroll
       for (int tb = 0; tb < TB; ++tb)
 #pragma unroll

@@ -39,3 +39,17 @@ def test_an_infinite_adapter_row_is_infinite(T, fp8):
     c["B"][1] = 1.0
     c["A_stack"][1023, 16 + 5] = float("inf")   # X is 1 there in every row
     assert (call(prc, c) == float("inf")).all()
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+@pytest.mark.parametrize("T,k,n", FORMS)
+def test_scales_and_agents_off_16_byte_lines(T, k, n, off):
+    """fp32 and int32 arrays need 4-byte alignment alone."""
+    k, n = (k + 15) // 16 * 16, (n + 15) // 16 * 16
+    c = exact_case(T + off, T, k, n, 3, 16, fp8=True)
+    for name in ("x_scale", "w_scale", "agent"):
+        wide = torch.zeros(len(c[name]) + 8, dtype=c[name].dtype, device="cuda")
+        wide[off:off + len(c[name])] = c[name]
+        c[name] = wide[off:off + len(c[name])]
+        assert c[name].data_ptr() % 16 == 4 * off
+    check(c)
