@@ -75,7 +75,8 @@ const char* prc_version(void);
  * materialise call, that 1 <= kv_len[b] <= s_cap and 0 <= positions[b][i] <
  * kv_len[b] (Sec. 2.2: every query sees a non-empty causal prefix of the
  * cache), and before an adapted projection that agent[i] < n_agents.  It reads
- * the verdict back, so each such call waits for its stream
+ * the verdict back, so each such call waits for its stream, and for other
+ * threads' calls on the device while their verdicts are read
  * (not usable under graph capture), and on a violation it launches nothing,
  * returns PRC_EDEVDATA and names the first offender (lowest request, then
  * lowest token; a kv_len fault before a position fault) in prc_last_error(). */

@@ -117,16 +117,19 @@ void rope_frequencies(double theta, int d, double* w2pi) {
 #if PRC_DEVICE_CHECKS
 // Checked build: before a call's kernels run, check the device-resident
 // kv_len and positions and read the verdict back (the call then waits for the
-// stream).  A failed check launches nothing and returns PRC_EDEVDATA.
+// stream).  A failed check launches nothing and returns PRC_EDEVDATA.  A device
+// has one result, which a call holds from its check's launch until it has read
+// the verdict: calls of other threads wait, whatever their streams.
 int32_t* g_check_ptr[kMaxDevices];
+std::mutex g_check_mu[kMaxDevices];
 
-prc_status check_array(const char* who, int32_t** res) {
+prc_status check_array(const char* who, int32_t** res, std::unique_lock<std::mutex>* held) {
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) {
     (void)hipGetLastError();
     return fail(PRC_EDEVICE, "no HIP device is current");
   }
-  std::lock_guard<std::mutex> lk(g_dev_mu);
+  std::unique_lock<std::mutex> lk(g_dev_mu);
   if (g_check_ptr[dev] == nullptr) {
     int32_t* p = nullptr;
     const hipError_t e = prc::device_checks_result(&p);
@@ -137,6 +140,8 @@ prc_status check_array(const char* who, int32_t** res) {
     g_check_ptr[dev] = p;
   }
   *res = g_check_ptr[dev];
+  lk.unlock();  // a call that waits for its stream holds up no other device
+  *held = std::unique_lock<std::mutex>(g_check_mu[dev]);
   return PRC_OK;
 }
 
@@ -151,22 +156,26 @@ prc_status read_check(const char* who, hipError_t e, const int32_t* res, hipStre
 prc_status device_data_check(const char* who, const int32_t* positions, const int32_t* kv_len, int batch, int n_tok,
                              int64_t s_cap, hipStream_t st) {
   int32_t* res = nullptr;
-  if (prc_status s = check_array(who, &res)) return s;
+  std::unique_lock<std::mutex> held;
+  if (prc_status s = check_array(who, &res, &held)) return s;
   int32_t h[4] = {0, 0, 0, 0};
   if (prc_status s = read_check(who, prc::launch_device_checks(positions, kv_len, batch, n_tok, s_cap, res, st), res, st, h)) return s;
   if (h[0] == 1)
     return fail(PRC_EDEVDATA, "%s: kv_len[%d]=%d outside [1, s_cap=%lld]", who, h[1], h[3], (long long)s_cap);
   if (h[0] == 2)
     return fail(PRC_EDEVDATA, "%s: positions[%d][%d]=%d outside [0, kv_len[%d])", who, h[1], h[2], h[3], h[1]);
+  if (h[0] != 0) return fail(PRC_ELAUNCH, "%s: device check gave an unknown verdict %d", who, h[0]);
   return PRC_OK;
 }
 
 prc_status agent_check(const char* who, const int32_t* agent, int64_t T, int n_agents, hipStream_t st) {
   int32_t* res = nullptr;
-  if (prc_status s = check_array(who, &res)) return s;
+  std::unique_lock<std::mutex> held;
+  if (prc_status s = check_array(who, &res, &held)) return s;
   int32_t h[4] = {0, 0, 0, 0};
   if (prc_status s = read_check(who, prc::launch_agent_checks(agent, T, n_agents, res, st), res, st, h)) return s;
   if (h[0] == 3) return fail(PRC_EDEVDATA, "%s: agent[%d]=%d is not below n_agents=%d", who, h[2], h[3], n_agents);
+  if (h[0] != 0) return fail(PRC_ELAUNCH, "%s: device check gave an unknown verdict %d", who, h[0]);
   return PRC_OK;
 }
 #endif

@@ -53,3 +53,33 @@ def test_scales_and_agents_off_16_byte_lines(T, k, n, off):
         c[name] = wide[off:off + len(c[name])]
         assert c[name].data_ptr() % 16 == 4 * off
     check(c)
+
+
+def test_checked_calls_of_two_threads_read_their_own_verdicts():
+    """One thread's agents past the last, another's valid ones, each on its own stream: none takes the other's."""
+    from concurrent.futures import ThreadPoolExecutor
+    from paper_2609_34054_amd.binding import use_checked_library
+    good, bad = (exact_case(i, 20, 256, 272, 3, 16) for i in range(2))
+    bad["agent"][7] = 3
+    want = exact_y(good)
+
+    def run(c, stream):
+        seen = []
+        with torch.cuda.stream(stream):
+            for _ in range(200):
+                try:
+                    seen.append(call(prc, c))
+                except prc.PrecacheError as e:
+                    seen.append(e)
+            stream.synchronize()
+        return seen
+
+    torch.cuda.synchronize()
+    use_checked_library(True)
+    try:
+        with ThreadPoolExecutor(2) as pool:
+            goods, bads = (f.result() for f in [pool.submit(run, c, torch.cuda.Stream()) for c in (good, bad)])
+    finally:
+        use_checked_library(False)
+    assert all(isinstance(e, prc.PrecacheError) and e.status_name == "PRC_EDEVDATA" and "agent[7]=3" in str(e) for e in bads)
+    assert all(torch.equal(y.double(), want) for y in goods)
