@@ -161,11 +161,12 @@ def _raw_stream(stream) -> int:
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _allocating_on(stream):
-    """Tensors made inside belong to `stream`: memory that its earlier work, and no other stream's, may still use."""
+def _allocating_on(stream, device):
+    """Tensors made inside belong to `stream` (of `device`, which a raw handle does not tell): memory that its earlier
+    work, and no other stream's, may still use."""
     if stream is None:
         return contextlib.nullcontext()
-    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device))
 
 
 def _on_gpu(t) -> bool:
@@ -622,7 +623,7 @@ def _norm(func, x, weight, residual, eps, y, y_scale, residual_out, fp8, stream)
     if _on_gpu(x) and x.dim() == 2:
         nat = _native()
         if y is None or (fp8 and y_scale is None) or (residual is not None and residual_out is None):
-            with _allocating_on(stream):
+            with _allocating_on(stream, x.device):
                 if y is None:
                     y = torch.empty(x.shape, dtype=kind, device=x.device)
                 if fp8 and y_scale is None:
@@ -640,7 +641,7 @@ def _norm(func, x, weight, residual, eps, y, y_scale, residual_out, fp8, stream)
     _rows("weight", weight, torch.bfloat16, (d,))
     if residual is not None:
         _rows("residual", residual, torch.bfloat16, (T, d))
-    with _allocating_on(stream):
+    with _allocating_on(stream, x.device):
         if y is None:
             y = torch.empty((T, d), dtype=kind, device=x.device)
         if fp8 and y_scale is None:
@@ -692,14 +693,14 @@ def _adapted(func, X, x_scale, W, w_scale, A_stack, B, agent, Y, workspace, stre
         nat = _native()
         out, ws, raw = Y, workspace, _raw_stream(stream)
         if out is None:
-            with _allocating_on(stream):
+            with _allocating_on(stream, X.device):
                 out = torch.empty((X.shape[0], W.shape[1]), dtype=torch.bfloat16, device=X.device)
         while True:
             st = nat.m.adapted(getattr(nat, func), nat.adapted_projection_workspace_size, fp8, X, x_scale, W, w_scale,
                                A_stack, B, agent, out, ws, torch._C._cuda_getDevice(), raw)
             if type(st) is not tuple:
                 break
-            with _allocating_on(stream):
+            with _allocating_on(stream, X.device):
                 ws = torch.empty(st[0], dtype=torch.uint8, device=X.device)
         if st is not None:
             if st:
@@ -726,7 +727,7 @@ def _adapted(func, X, x_scale, W, w_scale, A_stack, B, agent, Y, workspace, stre
         _rows("A_stack", A_stack, torch.bfloat16, (d_in, n_agents * rank), contiguous=True)
         _rows("agent", agent, torch.int32, (T,))
     if Y is None:
-        with _allocating_on(stream):
+        with _allocating_on(stream, X.device):
             Y = torch.empty((T, d_out), dtype=torch.bfloat16, device=X.device)
     _rows("Y", Y, torch.bfloat16, (T, d_out))
     if workspace is not None and not workspace.is_contiguous():
@@ -736,7 +737,7 @@ def _adapted(func, X, x_scale, W, w_scale, A_stack, B, agent, Y, workspace, stre
     with torch.cuda.device(dev):
         need = adapted_projection_workspace_size(T, d_in, d_out, n_agents, rank)
         if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
-            with _allocating_on(stream):
+            with _allocating_on(stream, dev):
                 workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
         tail = [_ptr(A_stack), _ptr(B), n_agents, rank, _ptr(agent), _ptr(Y), _ld(Y), _ptr(workspace), ws_bytes,
