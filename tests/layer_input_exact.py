@@ -12,7 +12,7 @@ BF = torch.bfloat16
 
 def exact_case(seed, T, k, n, N, r, fp8=False, wide=False, device="cuda"):
     """Inputs of one projection as keyword arguments.  A row of X has up to 40 nonzeros: some among the last 16 k,
-    some next to multiples of 32, the others anywhere.  ``wide``: the entries of X A_a need up to 14 bits and cancel
+    some next to multiples of 32, the others one in each twentieth of k.  ``wide``: the entries of X A_a need up to 14 bits and cancel
     in pairs of ranks to small ones."""
     g = torch.Generator().manual_seed(seed)
 
@@ -20,7 +20,8 @@ def exact_case(seed, T, k, n, N, r, fp8=False, wide=False, device="cuda"):
         return torch.randint(lo, hi + 1, shape, generator=g)
 
     edge = (32 * ints(0, (k - 1) // 32, T, 12) - ints(0, 1, T, 12)).clamp(0, k - 1)
-    at = torch.cat([ints(0, k - 1, T, 20), edge, k - 1 - ints(0, min(15, k - 1), T, 7), torch.full((T, 1), k - 1)], 1)
+    every = (k * (torch.arange(20) + torch.rand(T, 20, generator=g)) / 20).long().clamp(0, k - 1)   # each twentieth of k
+    at = torch.cat([every, edge, k - 1 - ints(0, min(15, k - 1), T, 7), torch.full((T, 1), k - 1)], 1)
     X = torch.zeros(T, k).scatter_(1, at, (2 * ints(0, 1, T, 40) - 1).float())
     X[:, k - 1] = 1.0
     W = 2.0 * ints(0, 1, k, n) - 1

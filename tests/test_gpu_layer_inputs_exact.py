@@ -41,6 +41,27 @@ def test_an_infinite_adapter_row_is_infinite(T, fp8):
     assert (call(prc, c) == float("inf")).all()
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,k,n,N,r", [
+    (1, 65536, 64, 2, 16), (3, 8192, 1024, 3, 32), (9, 65552, 144, 4, 64), (16, 32784, 272, 5, 8), (17, 65536, 64, 2, 16),
+    (40, 65488, 80, 3, 64), (130, 65536, 64, 2, 8), (640, 65536, 64, 2, 16), (700, 32784, 2064, 3, 32), (2500, 16400, 2064, 9, 64),
+    (4097, 32768, 256, 1, 16), (20, 1 << 21, 16, 1, 8), (70, 1 << 20, 32, 1, 16),
+])
+def test_long_sums_leave_nothing_out(T, k, n, N, r, fp8):
+    """Every slice of a long k, its end and the adapters: a bound on the roundings of a sum would hide them."""
+    print(f"project {T} {k} {n} {N} r{r} fp8={fp8}", flush=True)
+    for seed in range(3 if T < 32 else 1):
+        check(exact_case(T + k + r + seed, T, k, n, N, r, fp8))
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,k,n", FORMS)
+def test_projections_of_whole_numbers(T, k, n, fp8):
+    k, n = ((k + 15) // 16 * 16, (n + 15) // 16 * 16) if fp8 else (k, n)
+    for r, N in ((8, 12), (64, 3)):
+        check(exact_case(T + k + r, T, k, n, N, r, fp8))
+
+
 @pytest.mark.parametrize("off", [1, 2, 3])
 @pytest.mark.parametrize("T,k,n", FORMS)
 def test_scales_and_agents_off_16_byte_lines(T, k, n, off):
