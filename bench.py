@@ -625,8 +625,9 @@ def fused_projection(prc, w, dev, steps, warmup):
 def layer(prc, w, dev, steps, warmup):
     """The attention half of a layer with adapters on q and o too, step by step:
     residual sum and norm, (for a segment) K/V projection with LR rows, q of
-    each row's agent, attention over the shared cache, o, and the next norm in 8
-    bits with the q projection that reads it.  One record for the decode step
+    each row's agent, its rotation (left to the caller: library calls here),
+    attention over the shared cache, o, and the next norm in 8 bits with the q
+    projection that reads it.  One record for the decode step
     (a token of each request, each its own agent) and one for a segment of one
     agent; beside norm, q and o the same in library calls."""
     import torch
@@ -671,7 +672,17 @@ def layer(prc, w, dev, steps, warmup):
         kvl = torch.full((n_req,), kv, dtype=torch.int32, device=dev)
         y, s = prc.add_rms_norm(x, weight, res)
         q = prc.adapted_projection(y, Wq, A_q, B_q, agent)
-        c = dict(Q=q.view(n_req, n_tok, n_q, d), K_base=K, V_base=V, L_k=L_k, L_v=L_v, B_k=B_k, B_v=B_v, positions=pos, kv_len=kvl)
+        ang = pos.view(T, 1, 1).double() * w["theta"] ** (-2.0 * torch.arange(d // 2, device=dev, dtype=torch.float64) / d)
+        cos, sin, qr = ang.cos().float(), ang.sin().float(), torch.empty_like(q)
+
+        def rotate():
+            lo, hi = q.view(T, n_q, d).float().chunk(2, -1)
+            torch.cat([lo * cos - hi * sin, hi * cos + lo * sin], -1, out=rotated)
+            qr.view(T, n_q, d).copy_(rotated)
+
+        rotated = torch.empty(T, n_q, d, device=dev)
+        rotate()
+        c = dict(Q=qr.view(n_req, n_tok, n_q, d), K_base=K, V_base=V, L_k=L_k, L_v=L_v, B_k=B_k, B_v=B_v, positions=pos, kv_len=kvl)
         O = torch.empty_like(c["Q"])
         dims = prc.make_dims(c["Q"], K, L_k, L_v, B_k, B_v, w["theta"])
         ws = torch.empty(max(1, prc.workspace_size(dims)), dtype=torch.uint8, device=dev)
@@ -683,6 +694,7 @@ def layer(prc, w, dev, steps, warmup):
         runs = {
             "norm": lambda: prc.add_rms_norm(x, weight, res, y=y, residual_out=s),
             "q": lambda: prc.adapted_projection(y, Wq, A_q, B_q, agent, Y=q, workspace=pws),
+            "q_rotation_library": rotate,
             "attention": lambda: attn(prc, c, w["theta"], O, ws),
             "o": lambda: prc.adapted_projection(O.view(T, nq), Wo, A_o, B_o, agent, Y=o, workspace=pws),
             "norm_e4m3": lambda: prc.add_rms_norm_fp8(o, weight, s, y=y8, y_scale=ys, residual_out=s2),
@@ -693,7 +705,7 @@ def layer(prc, w, dev, steps, warmup):
                                                              tok_offset=kv - T, rope_theta=w["theta"])
 
         def step():
-            for k in ("norm", "kv", "q", "attention", "o"):
+            for k in ("norm", "kv", "q", "q_rotation_library", "attention", "o"):
                 if k in runs:
                     runs[k]()
 

@@ -436,7 +436,9 @@ prc_status add_rms_norm_fp8(const uint16_t* x, int64_t T, int64_t d, int64_t ld_
  *   agent    [T] int32, DEVICE memory, in any order.  A row whose entry is
  *            negative takes the base projection alone; so does one at or past
  *            N, which the checked build reports (PRC_EDEVDATA).
- *   Y        [T, d_out] bf16, row stride ld_y; must overlap no input.
+ *   Y        [T, d_out] bf16, row stride ld_y; must overlap no input.  Rows of q
+ *            are not rotated: lr_shared_attention reads them after the caller
+ *            has rotated each at its position.
  *   n_agents == 0: X W for every row; A_stack, B and agent may be NULL and
  *            rank is ignored.
  *   workspace  device scratch of at least adapted_projection_workspace_size

@@ -758,7 +758,8 @@ def adapted_projection(X, W, A_stack, B, agent, *, Y=None, workspace=None, strea
     ``A_stack [d_in, N*r]``, ``B [N, r, d_out]`` bf16 contiguous; ``agent [T]``
     int32, entries outside [0, N) (use -1) taking the base projection alone.
     ``A_stack``, ``B`` and ``agent`` None: ``X @ W``.  A workspace is allocated
-    when none (or too small a one) is given.
+    when none (or too small a one) is given.  Rows of q are not rotated; what
+    :func:`lr_shared_attention` reads, the caller rotates.
     """
     return _adapted("adapted_projection", X, None, W, None, A_stack, B, agent, Y, workspace, stream)
 
