@@ -1331,17 +1331,22 @@ hipError_t launch_mid(const ProjectArgs& a, int ksa, hipStream_t st) {
 
 // The time of slabs in `ks` slices, in microseconds: a stage takes 0.29 while a CU
 // has one workgroup and 0.56 with two (96 rows of 4096 x 4096 in bf16: one slice,
-// on half the CUs, 27.3 us, three 19.1; four, which do not run at once, 24.2), 1.8
-// times that in e4m3 if W's rows start inside 128-byte lines (320 rows of 5120 x
-// 7248: 55 us, as tiles 45; in bf16 664 rows of 1232 x 496 17.2 and 23.6), the
+// on half the CUs, 28.0 us, two 22.7, three 19.4; four, which do not run at once,
+// 23.9), twice that in e4m3, whose stages bring 24 KB instead of 16 (320 rows of
+// 5120 x 7168, rank 16: 47 us, as tiles 35; 20 rows of 14336 x 4096, where it adds
+// slices, 26.8 -> 18.7), the
 // stages together no less than W takes at the rate of a copy (24 rows of 4096 x
 // 14336: one slice 30.5 us, two 36.7); sums are written and read at 3.5 TB/s (256
 // rows of 1024 x 1024: three slices 10.8 us, seven 13.9), each row's B at 11.
+// It is off where some CUs alone have two workgroups: of the 96 rows above it takes
+// two slices, not three.  Counting two as 1.5 times one chose better there, but left
+// no room for the turns of rows of many agents (160 rows of 14336 x 4096 in bf16,
+// rank 64, eight agents: 77 -> 163 us).
 double slab_time(int64_t T, int64_t d_in, int64_t d_out, int rank, bool fp8, int cus, int ks) {
   const int64_t cw = fp8 ? 128 : 64, n = ((d_out + cw - 1) / cw + 1) * ((T + SL_T - 1) / SL_T) * ks, nk = (d_in + cw - 1) / cw;
   const int64_t rounds = (n + 2 * cus - 1) / (2 * cus);
   const double fill = n < cus ? 1.0 : (rounds > 1 ? 2.0 : (double)n / cus), out = (double)T * (double)d_out;
-  const double stages = (double)(rounds * ((nk + ks - 1) / ks)) * (0.29 + 0.27 * (fill - 1.0)) * (fp8 && d_out % cw != 0 ? 1.8 : 1.0);
+  const double stages = (double)(rounds * ((nk + ks - 1) / ks)) * (0.29 + 0.27 * (fill - 1.0)) * (fp8 ? 2.0 : 1.0);
   const double once = (double)d_in * (double)d_out * (fp8 ? 1.0 : 2.0) / 5e6;
   return 7.5 + (stages > once ? stages : once) + out * 8.0 * ks / 3.5e6 + out * 2.0 * rank / 11e6;
 }
@@ -1396,11 +1401,12 @@ int tile_form(int64_t T, int64_t d_in, int64_t d_out, int n_agents, bool fp8, in
 
 // Slabs or tiles.  Slabs fill the CUs where tiles would leave most idle, and form
 // the adapter rows beside the others, but read X and W more often and their sums
-// once more.  Measured for 96 to 512 rows of 1024 x 1024 to 14336 x 4096 and 4096
-// x 14336, in bf16 with rank 16 and e4m3 with rank 64: 4096 x 4096, 96 rows 19.1
-// us as slabs against 29.2, 512 rows 57.8 against 34.4; 14336 x 4096 in e4m3, 160
-// rows 35.6 against 61.9; 1100 rows of 4096 x 256 21.6 against 40.1.  Up to 64 rows always: less than a tile's.  Without adapters
-// (n_agents 0) it goes as with some of rank 16.
+// once more.  Measured for 96 to 480 rows of 1024 x 8192 to 14336 x 4096 and up to
+// 4000 of 4096 x 256, in both types with ranks 8 to 64: 4096 x 4096 in bf16, rank
+// 16, 96 rows 23.5 us as slabs against 30.1, 192 rows 25.8 against 30.0, 320 rows
+// 38.1 against 30.7, 512 rows 55.9 against 35.5; 14336 x 4096 in e4m3, 160 rows 42.8
+// against 65.8; 1100 rows of 4096 x 256 18.9 against 33.7.  Up to 64 rows always:
+// less than a tile's.  Without adapters (n_agents 0) it goes as with some of rank 16.
 constexpr int SL_MOST = 4096;  // bounds the workspace
 
 bool slabs_pay(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, bool fp8, int cus) {
@@ -1409,7 +1415,10 @@ bool slabs_pay(int64_t T, int64_t d_in, int64_t d_out, int n_agents, int rank, b
   const SlabPlan p = slab_plan(T, d_in, d_out, n_agents, rank, fp8, cus);
   double us;
   tile_form(T, d_in, d_out, 1, fp8, cus, &us);
-  return slab_time(T, d_in, d_out, rank, fp8, cus, p.ks) < us + 3.0 + 8.0 * (double)d_in / 4096.0;  // (the adapter rows' launch)
+  // The adapter rows' launch, and their longer expansion past rank 16 (320 rows of
+  // 2048 x 2048, rank 64: 18.8 us as slabs, 25.2 as tiles).
+  us += 6.0 + 5.0 * (double)d_in / 4096.0 + (rank > 16 ? (rank - 16) / 12.0 : 0.0);
+  return slab_time(T, d_in, d_out, rank, fp8, cus, p.ks) < us;
 }
 
 template <bool FP8>
