@@ -1338,14 +1338,15 @@ hipError_t launch_mid(const ProjectArgs& a, int ksa, hipStream_t st) {
 // stages together no less than W takes at the rate of a copy (24 rows of 4096 x
 // 14336: one slice 30.5 us, two 36.7); sums are written and read at 3.5 TB/s (256
 // rows of 1024 x 1024: three slices 10.8 us, seven 13.9), each row's B at 11.
-// It is off where some CUs alone have two workgroups: of the 96 rows above it takes
-// two slices, not three.  Counting two as 1.5 times one chose better there, but left
-// no room for the turns of rows of many agents (160 rows of 14336 x 4096 in bf16,
-// rank 64, eight agents: 77 -> 163 us).
+// A few CUs with two workgroups delay all, so those count as 1.3 at least (two
+// slices of the 96 rows are 260 workgroups; 256 rows in one slice are as many, 35.6
+// us, as tiles 31.9).  Counting two always as 1.5 times one leaves no room for the
+// turns of rows of many agents (160 rows of 14336 x 4096 in bf16, rank 64, eight
+// agents: 77 -> 163 us).
 double slab_time(int64_t T, int64_t d_in, int64_t d_out, int rank, bool fp8, int cus, int ks) {
   const int64_t cw = fp8 ? 128 : 64, n = ((d_out + cw - 1) / cw + 1) * ((T + SL_T - 1) / SL_T) * ks, nk = (d_in + cw - 1) / cw;
   const int64_t rounds = (n + 2 * cus - 1) / (2 * cus);
-  const double fill = n < cus ? 1.0 : (rounds > 1 ? 2.0 : (double)n / cus), out = (double)T * (double)d_out;
+  const double fill = n <= cus ? 1.0 : (rounds > 1 ? 2.0 : ((double)n / cus > 1.3 ? (double)n / cus : 1.3)), out = (double)T * (double)d_out;
   const double stages = (double)(rounds * ((nk + ks - 1) / ks)) * (0.29 + 0.27 * (fill - 1.0)) * (fp8 ? 2.0 : 1.0);
   const double once = (double)d_in * (double)d_out * (fp8 ? 1.0 : 2.0) / 5e6;
   return 7.5 + (stages > once ? stages : once) + out * 8.0 * ks / 3.5e6 + out * 2.0 * rank / 11e6;
@@ -1403,7 +1404,7 @@ int tile_form(int64_t T, int64_t d_in, int64_t d_out, int n_agents, bool fp8, in
 // the adapter rows beside the others, but read X and W more often and their sums
 // once more.  Measured for 96 to 480 rows of 1024 x 8192 to 14336 x 4096 and up to
 // 4000 of 4096 x 256, in both types with ranks 8 to 64: 4096 x 4096 in bf16, rank
-// 16, 96 rows 23.5 us as slabs against 30.1, 192 rows 25.8 against 30.0, 320 rows
+// 16, 96 rows 19.3 us as slabs against 30.1, 192 rows 25.8 against 30.0, 320 rows
 // 38.1 against 30.7, 512 rows 55.9 against 35.5; 14336 x 4096 in e4m3, 160 rows 42.8
 // against 65.8; 1100 rows of 4096 x 256 18.9 against 33.7.  Up to 64 rows always:
 // less than a tile's.  Without adapters (n_agents 0) it goes as with some of rank 16.
