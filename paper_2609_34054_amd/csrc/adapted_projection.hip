@@ -666,7 +666,7 @@ template <bool FP8, int NP, int TT, int CB, int TB>
 __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x16 (&acc)[CB][TB], char* lds, int64_t t0, int tw,
                                             int64_t c0, int cb0) {
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, h = lane >> 5, grp = lane >> 4, i16 = lane & 15;
+  const int l32 = lane & 31;
   const int R = a.rank, rp = R < 16 ? 16 : R, nc = rp / 8;  // ranks with padding; 16-byte chunks of a row
   // Agents of the tile's tokens (four or two a lane) and of this wave's.
   constexpr int NT = TT / 64;
@@ -729,8 +729,6 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
   char* bs = lds + 2 * part;
   static_assert(expand_agents<NP, TT>(32) == EX_A, "fewer at rank 64 alone");
   const int most = rp == 64 ? expand_agents<NP, TT>(64) : EX_A;
-  const int wk = 8 * h + i16 / 4, ws = swz_blocks<false, NP>(wk);
-  const int wo = wk * WRB + (grp & 1) * 32 + i16 % 4 * 8;
   for (bool first = true; any != 0; first = false) {
     int id[EX_A] = {-1, -1, -1, -1};
 #pragma unroll
@@ -750,8 +748,10 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
     for (int g = 0; g < EX_A; ++g) {
       if (id[g] < 0) break;
       const i32x4 rb = buffer_rsrc(a.B + (int64_t)id[g] * R * a.d_out, (int32_t)(R * a.d_out * 2));
+      int ln = lane;  // (as below)
+      asm volatile("" : "+v"(ln));
       for (int i = wv; i < rp * NP / 16; i += 8) {
-        const int b = i * 1024 + lane * 16, k = b / WRB, p = b % WRB / 64, in = b % 64 / 2;
+        const int b = i * 1024 + ln * 16, k = b / WRB, p = b % WRB / 64, in = b % 64 / 2;
         const int64_t col = c0 + (p ^ swz_blocks<false, NP>(k)) * 32 + in;
         lds_dma16(rb, bs + g * rp * WRB + i * 1024, k < R && col < a.d_out ? (int32_t)((k * a.d_out + col) * 2) : INT32_MIN, 0);
       }
@@ -762,6 +762,11 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
 #pragma unroll
     for (int g = 0; g < EX_A; ++g) {
       if (id[g] < 0) break;
+      // Addresses formed anew for each agent: those of all, kept, spill.
+      int ln = lane;
+      asm volatile("" : "+v"(ln));
+      const int r0 = tw + (ln & 31), hn = ln >> 5, wk = 8 * hn + (ln & 15) / 4, ws = swz_blocks<false, NP>(wk);
+      const int wo = wk * WRB + (ln >> 4 & 1) * 32 + (ln & 3) * 8;
       if constexpr (CB * TB >= 8) {
         // 128 sums a lane leave room for one block's fragments at a time (more
         // spills: 34 us against 23 at 4096 x 256 x 4096).
@@ -778,7 +783,7 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
             for (int kk = 0; kk < rp / 16; ++kk) {
               const char* p = bs + g * rp * WRB + wo + ((cb0 + cb) ^ ws) * 64 + 16 * kk * WRB;
               const u32x2 lo = lds_read_tr16(p), hi = lds_read_tr16(p + 4 * WRB);
-              const char* hp = lds + chunk(tw + 32 * tb + l32, 2 * kk + h);
+              const char* hp = lds + chunk(r0 + 32 * tb, 2 * kk + hn);
               u32x4 fh = *reinterpret_cast<const u32x4*>(hp), fl = *reinterpret_cast<const u32x4*>(hp + part);
               if (!mine) fh = fl = u32x4{0u, 0u, 0u, 0u};
               const bf16x8 fb = as_bf16x8(u32x4{lo[0], lo[1], hi[0], hi[1]});
@@ -791,13 +796,10 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
         }
         continue;
       }
-      // Addresses formed anew for each agent: those of all, kept, spill.
-      int r0 = tw + l32, w0 = wo;
-      asm volatile("" : "+v"(r0), "+v"(w0));
       auto add = [&](auto KR) {  // KR steps of 16 ranks
         constexpr int kr = decltype(KR)::value;
         const char* rows = lds + r0 * kr * 32;  // rows 32 further swizzle alike
-        const int hs = (kr == 1 ? h : (kr == 2 ? h ^ ((r0 >> 2) & 3) : h ^ ((r0 >> 1) & 7))) * 16;
+        const int hs = (kr == 1 ? hn : (kr == 2 ? hn ^ ((r0 >> 2) & 3) : hn ^ ((r0 >> 1) & 7))) * 16;
         // Both parts of one token block at a time: those of all spill.
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) {
@@ -812,7 +814,7 @@ __device__ __forceinline__ void expand_tile(const ProjectArgs& a, int ksa, f32x1
           }
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb) {
-            const char* p = bs + g * rp * WRB + w0 + ((cb0 + cb) ^ ws) * 64;
+            const char* p = bs + g * rp * WRB + wo + ((cb0 + cb) ^ ws) * 64;
             bf16x8 fb[kr];
 #pragma unroll
             for (int kk = 0; kk < kr; ++kk) {
