@@ -401,7 +401,8 @@ prc_status materialize_agent_kv(const lrsa_dims* dims, const uint16_t* K_base,
  * Requires d % 8 == 0, 8 <= d <= 65536, row strides >= d and multiples of 8,
  * eps >= 0 and finite, T < 2^31, T times each row stride at most 2^44
  * (PRC_EUNSUPPORTED otherwise), and outputs that overlap no input and each
- * other nowhere (but for the rows in place above).  T == 0 is a no-op.
+ * other nowhere (but for the rows in place above), from an array's first element
+ * to its last: column ranges of one buffer overlap.  T == 0 is a no-op.
  */
 prc_status add_rms_norm(const uint16_t* x, int64_t T, int64_t d, int64_t ld_x, const uint16_t* residual,
                         int64_t ld_res, const uint16_t* weight, float eps, uint16_t* residual_out,
@@ -436,7 +437,8 @@ prc_status add_rms_norm_fp8(const uint16_t* x, int64_t T, int64_t d, int64_t ld_
  *   agent    [T] int32, DEVICE memory, in any order.  A row whose entry is
  *            negative takes the base projection alone; so does one at or past
  *            N, which the checked build reports (PRC_EDEVDATA).
- *   Y        [T, d_out] bf16, row stride ld_y; must overlap no input.  Rows of q
+ *   Y        [T, d_out] bf16, row stride ld_y; must overlap no input (from first
+ *            element to last, the gaps between rows among them).  Rows of q
  *            are not rotated: lr_shared_attention reads them after the caller
  *            has rotated each at its position.
  *   n_agents == 0: X W for every row; A_stack, B and agent may be NULL and
@@ -471,7 +473,8 @@ prc_status adapted_projection(const uint16_t* X, int64_t T, int64_t d_in, int64_
  *   fp32.
  * Arithmetic besides: the matrix instructions sum eight e4m3 products at a time,
  * each cut to a multiple of 2^-13 of the largest one's power of two, before the
- * fp32 sums.
+ * fp32 sums; x_scale[i] * w_scale[j] is formed in fp32 and should be a normal
+ * number there (rows and columns of zeros aside).
  * Requires d_in, d_out and ld_x multiples of 16 besides.
  */
 prc_status adapted_projection_fp8(const uint8_t* X, const float* x_scale, int64_t T, int64_t d_in, int64_t ld_x,

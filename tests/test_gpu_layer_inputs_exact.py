@@ -76,6 +76,21 @@ def test_scales_and_agents_off_16_byte_lines(T, k, n, off):
     check(c)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("T,k,n", FORMS)
+def test_nothing_is_written_past_the_workspace_and_the_rows(T, k, n, fp8):
+    k, n = ((k + 15) // 16 * 16, (n + 15) // 16 * 16) if fp8 else (k, n)
+    for r, N in ((8, 12), (64, 3)):
+        c = exact_case(T + k + r, T, k, n, N, r, fp8)
+        size = prc.adapted_projection_workspace_size(T, k, n, N, r)
+        ws = torch.full((size + 4096,), 90, dtype=torch.uint8, device="cuda")
+        Y = torch.full((T + 5, n + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+        call(prc, c, Y=Y[2:T + 2, :n], workspace=ws[:size])
+        assert torch.all(ws[size:] == 90)
+        assert torch.equal(Y[2:T + 2, :n].double(), exact_y(c))
+        assert torch.all(Y[:2] == 7.0) and torch.all(Y[T + 2:] == 7.0) and torch.all(Y[:, n:] == 7.0)
+
+
 def test_checked_calls_of_two_threads_read_their_own_verdicts():
     """One thread's agents past the last, another's valid ones, each on its own stream: none takes the other's."""
     from concurrent.futures import ThreadPoolExecutor
