@@ -1134,8 +1134,9 @@ hipError_t launch_tiles(const ProjectArgs& a, int ksa, hipStream_t st) {
 // (each stage's first and second half; waves w and w + 4 share a SIMD, one's
 // reads beside the other's MFMAs).  Stages of 128 bytes of k a row come through
 // one ring.  At the end the two waves of a k pair exchange halves of their sums.
-// Loads bound it: 512 x 4096 x 4096 in bf16 27.5 us, 25 without the MFMAs (a CU
-// takes 128 bytes every other clock, and each tile 24 KB of them a stage).
+// 512 x 4096 x 4096 in bf16 takes 27.5 us, 25 without the MFMAs: its loads, their
+// waits and barriers bound it, at half the 64 bytes a clock that a CU takes of whole
+// lines in the tiles above (24 KB a stage would be 12 us; why is not known).
 constexpr int MD_T = 128;
 
 template <bool FP8, int NP>
