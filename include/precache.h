@@ -450,8 +450,8 @@ prc_status add_rms_norm_fp8(const uint16_t* x, int64_t T, int64_t d, int64_t ld_
  *            workspace for calls of several sizes is as large as the largest of
  *            their sizes.)
  * Arithmetic: bf16 inputs, fp32 sums; X A_a enters its product with B_a in fp32,
- * or (more than 64 rows) as the sum of two bf16 parts, to 2^-17 of it; Y is
- * rounded once.  What is
+ * or (tiles, of more than 64 rows) as the sum of two bf16 parts, to 2^-17 of it;
+ * Y is rounded once.  What is
  * infinite or NaN in one agent's A or B, or in one row of X, stays in the rows
  * that use it.  The same call gives the same bits on the same kind of device;
  * calls of other T can sum in another order.

@@ -638,8 +638,9 @@ __device__ __forceinline__ void scale_tile(const ProjectArgs& a, f32x16 (&acc)[C
 // parts and put into LDS, and each agent's rows of B_a beside them, laid out as
 // the weights are.  A product is added to the tokens of its agent alone, so that
 // what is infinite or NaN in an adapter stays in the rows that use it.  The second
-// part costs 4096 x 4096 x 4096 in bf16 of runs nothing at rank 16 and 8 of 159 us
-// at rank 64, 2048 x 5120 x 5120 in e4m3, rank 64, 0.6 of 67.5.
+// part costs 4096 x 4096 x 4096 in bf16 nothing at rank 16 and 3 of 146 us at rank
+// 64 where rows come in runs, 16 of 263 at rank 16 where 32 agents mix; 2048 x 5120 x
+// 5120 in e4m3, rank 64, 0.5 of 67.
 constexpr int EX_A = 4;  // agents at a time
 constexpr int EX_LDS = 160 * 1024;
 
